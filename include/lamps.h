@@ -28,7 +28,7 @@
  *   - "device" pointers are HIP device memory of the current device; "host"
  *     pointers are ordinary process memory unless marked pinned.
  *   - Arguments that live in device memory (block_table, ctx_lens,
- *     running_mask) are NOT validated: no call synchronises with the device.
+ *     running_mask, lengths and ids) are NOT validated: no call synchronises with the device.
  *     The kernels keep these mistakes harmless (no access outside the pools;
  *     the affected rows are meaningless): a context length beyond
  *     max_blocks_per_req * block_size is clamped to the row by the decode
@@ -38,20 +38,21 @@
  *     lamps_validate_args checks all of this on request (it synchronises).
  *   - A context is not thread-safe; calls on it must be serialised -- with one
  *     exception: the compute-stream calls (lamps_decode_attn, lamps_kv_append,
- *     lamps_kv_append_tokens, lamps_prefill_attn) read nothing of the context that
- *     ever changes, so ONE thread may make them while ONE other thread makes
+ *     lamps_kv_append_tokens, lamps_prefill_attn, lamps_decode_attn_window,
+ *     lamps_prefill_attn_window, lamps_rope_append, lamps_rope_append_tokens,
+ *     lamps_batch_tables) read nothing of the context that ever changes, so ONE thread may make them while ONE other thread makes
  *     all the block-management and swap calls (alloc, free, swap, ticket, wait
  *     calls).  lamps_last_error then reports the most recent failure of either;
  *     read it from the thread whose call failed, before its next call.
- *   - lamps_decode_attn, lamps_kv_append, lamps_kv_append_tokens and
- *     lamps_prefill_attn enqueue kernels on the compute stream and nothing else
+ *   - The compute-stream calls just named enqueue kernels on the compute stream and nothing else
  *     (no memset, no copy, no allocation, no host wait): once each has run
  *     eagerly on the device, a caller may record them into a HIP graph by stream
  *     capture and replay a whole decode iteration.  The swap calls use events
  *     and copies on the side streams and are not meant for capture.
  *   - The decode and prefill kernels of one context share its workspace
- *     (lamps_workspace_bytes): all of its lamps_decode_attn and
- *     lamps_prefill_attn work, eager and replayed, must run in one order -- on
+ *     (lamps_workspace_bytes): all of its lamps_decode_attn, lamps_prefill_attn,
+ *     lamps_decode_attn_window and lamps_prefill_attn_window work, eager and
+ *     replayed, must run in one order -- on
  *     the compute stream, or on other streams behind one another by events.  A
  *     replay beside a call or another replay of the same context overwrites
  *     its partial results and gives wrong rows, with no error.  (Two contexts
@@ -328,6 +329,145 @@ int lamps_kv_append_tokens(lamps_ctx *ctx, int32_t layer, int32_t n_req, int32_t
 int lamps_prefill_attn(lamps_ctx *ctx, int32_t layer, int32_t n_req, int32_t total_tokens,
                        int32_t max_new_tokens, const void *q, const int32_t *q_start,
                        const int32_t *block_table, const int32_t *ctx_lens, void *out);
+
+/* ---- attention over a window of the last positions and the first few ---- */
+
+/* lamps_decode_attn where the new token at the end of each request's context sees
+ * only the last `window` cached positions (its own among them) and the first
+ * `sinks`: position t counts if t < ctx_lens[r] and (t >= ctx_lens[r] - window or
+ * t < sinks).  A window of ctx_lens[r] and more is lamps_decode_attn's equation.
+ * Keys and values that do not count are never part of a result, whatever they are
+ * (NaN and infinities among them), and table entries of blocks in which no position
+ * counts are never read: such a block may have been given back (lamps_free_blocks)
+ * and its entry hold anything.  The rest -- rows that do not run, empty contexts,
+ * types, order, reproducibility, workspace -- is as for lamps_decode_attn, except
+ * that a score, key or value that counts and is no finite number makes the row (or,
+ * for a value, its element) no finite number either.
+ *   q, out        device, [batch][H][d_h] dtype, 16-byte aligned
+ * Errors: INVALID (null, alignment, window < 1, sinks < 0), RANGE (layer, batch). */
+int lamps_decode_attn_window(lamps_ctx *ctx, int32_t layer, int32_t batch, int32_t window,
+                             int32_t sinks, const void *q, const int32_t *block_table,
+                             const int32_t *ctx_lens, const uint8_t *running_mask, void *out);
+
+/* lamps_prefill_attn where the new token at position p sees the cached positions
+ * t <= p with t > p - window or t < sinks.  What counts for none of a request's new
+ * tokens is not read, nor are the table entries of blocks that hold nothing else;
+ * what does not count for one of them has no part in its row.  Rows, arguments,
+ * max_new_tokens, types, order and workspace are as for lamps_prefill_attn (bf16:
+ * weights rounded to bf16 before the second product, except by a wavefront per token).
+ * Errors: INVALID (null, alignment, window < 1, sinks < 0), RANGE (layer, n_req >
+ * max_batch, negative sizes). */
+int lamps_prefill_attn_window(lamps_ctx *ctx, int32_t layer, int32_t n_req, int32_t total_tokens,
+                              int32_t max_new_tokens, int32_t window, int32_t sinks, const void *q,
+                              const int32_t *q_start, const int32_t *block_table,
+                              const int32_t *ctx_lens, void *out);
+
+/* ---- queries and keys normalised and rotated on their way to attention and cache ---- */
+
+/* Which two dims of the first rotary_dim of a head are turned together:
+ *   HALVES      (i, i + rotary_dim / 2)      NEIGHBOURS  (2 i, 2 i + 1) */
+typedef enum { LAMPS_ROPE_HALVES = 0, LAMPS_ROPE_NEIGHBOURS = 1 } lamps_rope_pairs;
+
+/* How the two calls below turn one head x of a query or key at position p:
+ *   with `normalise`   x <- x / sqrt(mean(x^2) + norm_eps) * weight   (over the head's d_h dims)
+ *   then for every pair (a, b), the i-th,   with  u = p * frequencies[i]
+ *       (a, b) <- amplitude * (a cos u - b sin u,  a sin u + b cos u)
+ * in fp32 (the angle in fp64, so far positions keep their accuracy), rounded once
+ * at the end.  Dims from rotary_dim on are not turned. */
+typedef struct {
+    int32_t rotary_dim;         /* 0 (no rotation) .. head_dim, a multiple of 16      */
+    int32_t pairs;              /* lamps_rope_pairs                                   */
+    int32_t normalise;          /* != 0: each head of q and k is normalised first     */
+    float norm_eps;             /* >= 0                                               */
+    float amplitude;            /* 0 => 1                                             */
+    const double *frequencies;  /* device, [rotary_dim / 2], radians per position, 8-byte
+                                   aligned (lamps_rope_frequencies); NULL if none     */
+    const void *q_weight;       /* device, [d_h] dtype, 16-byte aligned; NULL => ones */
+    const void *k_weight;
+} lamps_rope;
+
+/* Frequencies of the usual forms, in radians per position, written to `frequencies`
+ * (HOST, [rotary_dim / 2]; the caller copies them to the device).  With
+ * f_i = base^(-2 i / rotary_dim):
+ *   UNSCALED  f_i
+ *   LINEAR    f_i / factor            (positions interpolated)
+ *   BASE      f_i of base * factor^(rotary_dim / (rotary_dim - 2))
+ *   BY_PARTS  g f_i + (1 - g) f_i / factor, with the turns of a pair over the length
+ *             the model was trained on, n = original_positions f_i / (2 pi), and
+ *             g = (n - low_turns) / (high_turns - low_turns) held within [0, 1]
+ * Pure host function.  Errors: INVALID (null, rotary_dim no positive multiple of 16,
+ * scaling, base <= 1, factor < 1, and for BY_PARTS original_positions <= 0 or
+ * high_turns <= low_turns; numbers that are not finite). */
+typedef enum { LAMPS_ROPE_UNSCALED = 0, LAMPS_ROPE_LINEAR = 1, LAMPS_ROPE_BASE = 2, LAMPS_ROPE_BY_PARTS = 3 } lamps_rope_scaling;
+int lamps_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor,
+                           double original_positions, double low_turns, double high_turns,
+                           double *frequencies);
+
+/* lamps_kv_append for vectors as the projections leave them: for every request
+ * r < batch with running_mask[r] != 0 and p = ctx_lens[r], q_out[r] = the queries
+ * q[r] normalised and turned to position p, and the keys k_new[r], treated the same
+ * way, and the values v_new[r], as they are, go to cached position p of `layer`.
+ * advance, table entries and lengths are as for lamps_kv_append; a position outside
+ * the table row, or a block id outside the pool, writes nothing at all of that
+ * request.  Rows of q_out of requests that do not run are not written.
+ *   rope           host; what it points to is device memory
+ *   q              device, [batch] rows of [H][d_h], q_stride elements apart
+ *   k_new, v_new   device, [batch] rows of [H_kv][d_h], k_stride / v_stride apart
+ *                  (so that the three may be parts of one projection's rows; 0 => the
+ *                  rows follow each other).  16-byte aligned, strides multiples of
+ *                  16 bytes and no less than a row.
+ *   q_out          device, [batch][H][d_h], 16-byte aligned; may be q itself where
+ *                  q's rows follow each other, and may not overlap the inputs otherwise
+ * Errors: INVALID (null, alignment, strides, overlap, rope), RANGE (layer, batch). */
+int lamps_rope_append(lamps_ctx *ctx, int32_t layer, int32_t batch, const lamps_rope *rope,
+                      const void *q, int64_t q_stride, const void *k_new, int64_t k_stride,
+                      const void *v_new, int64_t v_stride, const int32_t *block_table,
+                      int32_t *ctx_lens, const uint8_t *running_mask, int32_t advance, void *q_out);
+
+/* The same for several new tokens per request, rows and positions as for
+ * lamps_kv_append_tokens (row q_start[r] + i is position ctx_lens[r] - n_r + i).
+ * A block id outside the pool writes nothing of the rows whose positions lie in it;
+ * rows past q_start[n_req] are not written.
+ * Errors: INVALID (null, alignment, strides, overlap, rope), RANGE (layer, n_req >
+ * max_batch, negative sizes). */
+int lamps_rope_append_tokens(lamps_ctx *ctx, int32_t layer, int32_t n_req, int32_t total_tokens,
+                             const lamps_rope *rope, const void *q, int64_t q_stride,
+                             const void *k_new, int64_t k_stride, const void *v_new,
+                             int64_t v_stride, const int32_t *q_start, const int32_t *block_table,
+                             const int32_t *ctx_lens, void *q_out);
+
+/* ---- a batch's tables, made on the device from the lengths ---- */
+
+/* What the calls above want to know of a batch, enqueued on the compute stream:
+ * request r has cached[r] positions and brings new_tokens[r] more.  Its row needs
+ * ceil((cached + new) / block_size) blocks; with grow != 0 it holds the
+ * ceil(cached / block_size) of them that its cached positions lie in already, which
+ * stay as they are, with grow == 0 none.  The others are taken from block_ids, in
+ * order, request after request.
+ *   cached, new_tokens  device, int32 [n_req]
+ *   block_ids           device, int32 [n_ids] (NULL if n_ids == 0), n_ids <= num_blocks
+ *   block_table         device, int32 [n_req][max_blocks_per_req]: the entries taken are
+ *                       written, and -1 behind them to the end of the row
+ *   ctx_lens            device, int32 [n_req]: cached + new
+ *   q_start             device, int32 [n_req + 1]: the rows of the new tokens begin there,
+ *                       q_start[n_req] is how many there are
+ *   slots               device, int64 [total_tokens] or NULL: row n's place in the cache,
+ *                       block id * block_size + slot (-1: no such row, or an entry
+ *                       that names no block of the pool)
+ *   report              device, int32 [4] or NULL: ids taken, requests not served, the
+ *                       lowest of them (-1: none), new tokens of those served
+ * A request is not served if its lengths are negative or their sum is beyond the row,
+ * if it needs blocks and the ids, dealt in order, do not reach to the last of them, or
+ * if it brings tokens and these, counted in order, go beyond total_tokens.  Such a
+ * request has length 0 and no rows, and its table row is not written.  The ids that it
+ * would have taken stay with it: the next request begins behind them.
+ * The outputs may overlap neither each other nor the inputs.
+ * Errors: INVALID (null, overlap), RANGE (n_req > max_batch, negative sizes, n_ids >
+ * num_blocks). */
+int lamps_batch_tables(lamps_ctx *ctx, int32_t n_req, int32_t total_tokens, const int32_t *cached,
+                       const int32_t *new_tokens, const int32_t *block_ids, int32_t n_ids,
+                       int32_t grow, int32_t *block_table, int32_t *ctx_lens, int32_t *q_start,
+                       int64_t *slots, int32_t *report);
 
 /* ---- Swap handling strategy (Section 1; Section 4.2) ---- */
 

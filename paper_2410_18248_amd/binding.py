@@ -9,6 +9,8 @@ import os
 
 LAMPS_F32, LAMPS_BF16 = 0, 1
 LAMPS_LAYOUT_PLAIN, LAMPS_LAYOUT_TILED = 0, 1
+LAMPS_ROPE_HALVES, LAMPS_ROPE_NEIGHBOURS = 0, 1
+LAMPS_ROPE_UNSCALED, LAMPS_ROPE_LINEAR, LAMPS_ROPE_BASE, LAMPS_ROPE_BY_PARTS = range(4)
 
 STATUS = {0: "LAMPS_OK", -1: "LAMPS_ERR_INVALID", -2: "LAMPS_ERR_RANGE", -3: "LAMPS_ERR_DUP",
           -4: "LAMPS_ERR_DOUBLE_FREE", -5: "LAMPS_ERR_BUSY", -6: "LAMPS_ERR_NOMEM",
@@ -35,6 +37,19 @@ class LampsConfig(ctypes.Structure):
                 ("part_tokens", ctypes.c_int32), ("staging_bytes", ctypes.c_int64),
                 ("direct_copy_bytes", ctypes.c_int64), ("zero_copy_workgroups", ctypes.c_int32),
                 ("max_swaps_in_flight", ctypes.c_int32)]
+
+
+class LampsRope(ctypes.Structure):
+    """``lamps_rope``.  `frequencies`, `q_weight` and `k_weight` are device memory, which this object keeps alive where it is a tensor."""
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("pairs", ctypes.c_int32), ("normalise", ctypes.c_int32),
+                ("norm_eps", ctypes.c_float), ("amplitude", ctypes.c_float), ("frequencies", ctypes.c_void_p),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p)]
+
+    def __init__(self, rotary_dim, pairs=LAMPS_ROPE_HALVES, frequencies=None, amplitude=0.0, normalise=False, norm_eps=1e-6,
+                 q_weight=None, k_weight=None):
+        super().__init__(rotary_dim, pairs, 1 if normalise else 0, norm_eps, amplitude, _ptr(frequencies) or None,
+                         _ptr(q_weight) or None, _ptr(k_weight) or None)
+        self._keep = (frequencies, q_weight, k_weight)
 
 
 def lib_path():
@@ -64,6 +79,7 @@ def load_library():
         raise ImportError("liblamps.so is not built: run `python -m paper_2410_18248_amd.build`")
     lib = ctypes.CDLL(path)
     vp, i32, u64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64
+    i64, f64 = ctypes.c_int64, ctypes.c_double
     cfgp = ctypes.POINTER(LampsConfig)
     for name in ("lamps_kv_bytes_per_token", "lamps_block_bytes", "lamps_pool_bytes",
                  "lamps_workspace_bytes"):
@@ -80,6 +96,12 @@ def load_library():
         "lamps_kv_append": [vp, i32, i32, vp, vp, vp, vp, vp, i32],
         "lamps_kv_append_tokens": [vp, i32, i32, i32, vp, vp, vp, vp, vp],
         "lamps_prefill_attn": [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp],
+        "lamps_decode_attn_window": [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp],
+        "lamps_prefill_attn_window": [vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp],
+        "lamps_rope_frequencies": [i32, f64, i32, f64, f64, f64, f64, vp],
+        "lamps_rope_append": [vp, i32, i32, ctypes.POINTER(LampsRope), vp, i64, vp, i64, vp, i64, vp, vp, vp, i32, vp],
+        "lamps_rope_append_tokens": [vp, i32, i32, i32, ctypes.POINTER(LampsRope), vp, i64, vp, i64, vp, i64, vp, vp, vp, vp],
+        "lamps_batch_tables": [vp, i32, i32, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp],
         "lamps_swap_out": [vp, vp, i32, vp, ctypes.POINTER(u64)],
         "lamps_swap_in": [vp, vp, vp, i32, ctypes.POINTER(u64)],
         "lamps_swap_out_layered": [vp, vp, i32, vp, ctypes.POINTER(u64)],
@@ -276,6 +298,18 @@ def lamps_workspace_bytes(cfg):
     return load_library().lamps_workspace_bytes(ctypes.byref(cfg))
 
 
+def lamps_rope_frequencies(rotary_dim, base, scaling=LAMPS_ROPE_UNSCALED, factor=1.0, original_positions=0.0, low_turns=0.0,
+                           high_turns=0.0):
+    """The frequencies as a list; the caller makes a float64 tensor on the device of them.  None for rotary_dim 0: an empty list."""
+    if rotary_dim == 0:
+        return []
+    f = (ctypes.c_double * max(rotary_dim // 2, 1))()
+    rc = load_library().lamps_rope_frequencies(rotary_dim, base, scaling, factor, original_positions, low_turns, high_turns, f)
+    if rc < 0:
+        raise LampsError(rc, "lamps_rope_frequencies")
+    return list(f)
+
+
 def lamps_decode_attn_static(cfg, compute_stream, layer, batch, q, k_pool, v_pool, block_table, ctx_lens,
                              running_mask, out):
     lib = load_library()
@@ -343,6 +377,34 @@ class Lamps:
         self._check(self.lib.lamps_prefill_attn(self.h, layer, n_req, total_tokens, max_new_tokens, _ptr(q),
                                                 _ptr(q_start), _ptr(block_table), _ptr(ctx_lens),
                                                 _ptr(out)))
+
+    def decode_attn_window(self, layer, batch, window, sinks, q, block_table, ctx_lens, running_mask, out):
+        self._check(self.lib.lamps_decode_attn_window(self.h, layer, batch, window, sinks, _ptr(q), _ptr(block_table),
+                                                      _ptr(ctx_lens), _ptr(running_mask), _ptr(out)))
+
+    def prefill_attn_window(self, layer, n_req, total_tokens, window, sinks, q, q_start, block_table, ctx_lens, out,
+                            max_new_tokens=0):
+        self._check(self.lib.lamps_prefill_attn_window(self.h, layer, n_req, total_tokens, max_new_tokens, window, sinks,
+                                                       _ptr(q), _ptr(q_start), _ptr(block_table), _ptr(ctx_lens), _ptr(out)))
+
+    def rope_append(self, layer, batch, rope, q, k_new, v_new, block_table, ctx_lens, running_mask, advance, q_out,
+                    q_stride=0, k_stride=0, v_stride=0):
+        """Strides in elements; 0: rows follow each other (they are not taken from a tensor's own strides)."""
+        self._check(self.lib.lamps_rope_append(self.h, layer, batch, rope, _ptr(q), q_stride, _ptr(k_new), k_stride, _ptr(v_new),
+                                               v_stride, _ptr(block_table), _ptr(ctx_lens), _ptr(running_mask),
+                                               1 if advance else 0, _ptr(q_out)))
+
+    def rope_append_tokens(self, layer, n_req, total_tokens, rope, q, k_new, v_new, q_start, block_table, ctx_lens, q_out,
+                           q_stride=0, k_stride=0, v_stride=0):
+        self._check(self.lib.lamps_rope_append_tokens(self.h, layer, n_req, total_tokens, rope, _ptr(q), q_stride, _ptr(k_new),
+                                                      k_stride, _ptr(v_new), v_stride, _ptr(q_start), _ptr(block_table),
+                                                      _ptr(ctx_lens), _ptr(q_out)))
+
+    def batch_tables(self, n_req, total_tokens, cached, new_tokens, block_ids, n_ids, grow, block_table, ctx_lens, q_start,
+                     slots=None, report=None):
+        self._check(self.lib.lamps_batch_tables(self.h, n_req, total_tokens, _ptr(cached), _ptr(new_tokens), _ptr(block_ids),
+                                                n_ids, 1 if grow else 0, _ptr(block_table), _ptr(ctx_lens), _ptr(q_start),
+                                                _ptr(slots), _ptr(report)))
 
     def swap_out(self, block_ids, host_buf, layered=False):
         arr, n = _ids(block_ids)

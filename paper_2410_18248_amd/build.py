@@ -25,8 +25,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblamps.so")
-SOURCES = ["decode_attn.hip", "block_copy.hip", "kv_append.hip", "prefill_attn.hip", "validate.hip", "lamps.cpp",
-           "sched.cpp"]
+SOURCES = ["decode_attn.hip", "block_copy.hip", "kv_append.hip", "prefill_attn.hip", "window_attn.hip", "rope_append.hip",
+           "batch_tables.hip", "validate.hip", "lamps.cpp", "sched.cpp"]
 # the scheduler's times are compared bit for bit with a plain evaluation of the same formulas:
 # no fused multiply-adds in its host code
 PER_SOURCE = {"sched.cpp": ["-ffp-contract=off"],
@@ -35,7 +35,8 @@ PER_SOURCE = {"sched.cpp": ["-ffp-contract=off"],
               # tokens in the decode kernel), and mfma_f32_16x16x32_bf16 issues every 16 cycles instead of
               # every 30-47 (measured)
               "decode_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-              "prefill_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+              "prefill_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+              "window_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",

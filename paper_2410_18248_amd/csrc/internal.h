@@ -94,6 +94,46 @@ struct PrefillArgs {
 // the positions up to and including its own.
 hipError_t launch_prefill(const PrefillArgs &a, hipStream_t stream);
 
+// Decode and many-token attention over the last `window` positions and the first `sinks` of what lamps_decode_attn and lamps_prefill_attn
+// attend to.
+struct WindowArgs {
+    DecodeArgs d;                // prefill: q and out are [total_tokens][H][D]; batch = number of requests
+    const int32_t *q_start;      // [batch + 1]; nullptr: one new token per request, the last of its context
+    int32_t window, sinks;
+    int32_t total_tokens, max_new_tokens, force_rows;   // as in PrefillArgs
+    int32_t parts;               // workgroups that share a range (filled in by the launcher)
+};
+hipError_t launch_decode_window(const WindowArgs &a, hipStream_t stream);
+hipError_t launch_prefill_window(const WindowArgs &a, hipStream_t stream);
+
+struct RopeArgs {
+    const void *q, *k_new, *v_new;   // rows of [H or H_kv][D], the strides apart
+    void *q_out;                     // [rows][H][D]
+    void *k_pool, *v_pool;
+    const double *frequencies;       // [rotary_dim / 2]
+    const void *q_weight, *k_weight; // [D] or nullptr
+    const int32_t *block_table;
+    int32_t *ctx_lens;               // [batch]; incremented for running requests if advance
+    const uint8_t *running;          // [batch] (one token per request)
+    const int32_t *q_start;          // [batch + 1] (many tokens)
+    int64_t q_stride, k_stride, v_stride;   // elements
+    float amplitude, norm_eps, inv_dim;
+    int32_t rotary_dim, neighbours, normalise, advance, total_tokens;
+    int32_t batch, bf16, layer, num_layers, num_q_heads, num_kv_heads, head_dim, block_size, log2_block_size, max_blocks, num_blocks;
+    int32_t heads_each;              // kv heads of a workgroup (filled in by the launcher)
+};
+// total_tokens < 0: one new token per running request
+hipError_t launch_rope_append(const RopeArgs &a, int total_tokens, int tiled, hipStream_t stream);
+
+struct TableArgs {
+    const int32_t *cached, *new_tokens, *block_ids;
+    int32_t *block_table, *ctx_lens, *q_start, *report;
+    int64_t *slots;
+    int32_t n_req, total_tokens, n_ids, grow, max_blocks, num_blocks, log2_block_size;
+    int32_t table_items, wide;       // filled in by the launcher
+};
+hipError_t launch_batch_tables(TableArgs a, hipStream_t stream);
+
 // Checks the device-resident arguments of a decode call: for every request r < batch, whether
 // ctx_lens[r] is negative or beyond the block-table row, and, for running requests, whether any
 // block-table entry its context uses lies outside [0, num_blocks).  result (device, 4 + 2 * batch

@@ -196,6 +196,82 @@ void fill_decode_args(lamps_ctx *c, lamps::DecodeArgs *pa, int32_t layer, int32_
     a.layer = layer;
 }
 
+bool overlap(const void *a, size_t na, const void *b, size_t nb)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && na && nb && x < y + nb && y < x + na;
+}
+
+// What is wrong with the rope and the rows of a rope_append call, or nullptr; fills in `a` but for the call's lengths.
+const char *fill_rope_args(lamps_ctx *c, lamps::RopeArgs *pa, int32_t layer, int32_t batch, int32_t rows, const lamps_rope *rope,
+                           const void *q, int64_t q_stride, const void *k_new, int64_t k_stride, const void *v_new, int64_t v_stride,
+                           const int32_t *block_table, const int32_t *ctx_lens, void *q_out)
+{
+    if (!rope || !q || !k_new || !v_new || !block_table || !ctx_lens || !q_out) return "null argument";
+    const lamps_config &g = c->cfg;
+    const int64_t es = (int64_t)c->d.elem, qrow = (int64_t)g.num_q_heads * g.head_dim, krow = (int64_t)g.num_kv_heads * g.head_dim;
+    if (((uintptr_t)q | (uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)q_out) & 15) return "q, k_new, v_new and q_out must be 16-byte aligned";
+    if (rope->rotary_dim < 0 || rope->rotary_dim > g.head_dim || rope->rotary_dim % 16 != 0) return "rotary_dim must be a multiple of 16 in [0, head_dim]";
+    if (rope->pairs != LAMPS_ROPE_HALVES && rope->pairs != LAMPS_ROPE_NEIGHBOURS) return "pairs must be LAMPS_ROPE_HALVES or LAMPS_ROPE_NEIGHBOURS";
+    if (rope->rotary_dim > 0 && !rope->frequencies) return "frequencies is null";
+    if ((uintptr_t)rope->frequencies & 7) return "frequencies must be 8-byte aligned";
+    if (((uintptr_t)rope->q_weight | (uintptr_t)rope->k_weight) & 15) return "q_weight and k_weight must be 16-byte aligned";
+    if (!std::isfinite(rope->amplitude)) return "amplitude is no finite number";
+    if (rope->normalise && !(rope->norm_eps >= 0.f && std::isfinite(rope->norm_eps))) return "norm_eps must be a finite number of 0 and more";
+    if (q_stride == 0) q_stride = qrow;
+    if (k_stride == 0) k_stride = krow;
+    if (v_stride == 0) v_stride = krow;
+    const int64_t most = (int64_t)1 << 40;
+    if (q_stride < qrow || k_stride < krow || v_stride < krow || q_stride > most || k_stride > most || v_stride > most)
+        return "a stride is less than a row";
+    if (q_stride * es % 16 != 0 || k_stride * es % 16 != 0 || v_stride * es % 16 != 0) return "strides must be multiples of 16 bytes";
+    if (rows > 0) {
+        const size_t out = (size_t)rows * qrow * es;
+        const auto span = [&](int64_t stride, int64_t row) { return (size_t)(((int64_t)(rows - 1) * stride + row) * es); };
+        if (overlap(q_out, out, k_new, span(k_stride, krow)) || overlap(q_out, out, v_new, span(v_stride, krow)) ||
+            (overlap(q_out, out, q, span(q_stride, qrow)) && !(q_out == q && q_stride == qrow)))
+            return "q_out overlaps the inputs";
+    }
+    lamps::RopeArgs &a = *pa;
+    a.q = q;
+    a.k_new = k_new;
+    a.v_new = v_new;
+    a.q_out = q_out;
+    a.k_pool = c->k_pool;
+    a.v_pool = c->v_pool;
+    a.frequencies = rope->frequencies;
+    a.q_weight = rope->q_weight;
+    a.k_weight = rope->k_weight;
+    a.block_table = block_table;
+    a.ctx_lens = const_cast<int32_t *>(ctx_lens);         // written with advance only
+    a.running = nullptr;
+    a.q_start = nullptr;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.amplitude = rope->amplitude != 0.f ? rope->amplitude : 1.f;
+    a.norm_eps = rope->norm_eps;
+    a.inv_dim = 1.f / (float)g.head_dim;
+    a.rotary_dim = rope->rotary_dim;
+    a.neighbours = rope->pairs == LAMPS_ROPE_NEIGHBOURS;
+    a.normalise = rope->normalise != 0;
+    a.advance = 0;
+    a.total_tokens = rows;
+    a.batch = batch;
+    a.bf16 = g.dtype == LAMPS_BF16;
+    a.layer = layer;
+    a.num_layers = g.num_layers;
+    a.num_q_heads = g.num_q_heads;
+    a.num_kv_heads = g.num_kv_heads;
+    a.head_dim = g.head_dim;
+    a.block_size = g.block_size;
+    a.log2_block_size = c->d.log2_bs;
+    a.max_blocks = g.max_blocks_per_req;
+    a.num_blocks = g.num_blocks;
+    a.heads_each = 1;
+    return nullptr;
+}
+
 int fail(lamps_ctx *c, int code, const std::string &msg)
 {
     if (c) {
@@ -804,6 +880,181 @@ int lamps_prefill_attn(lamps_ctx *c, int32_t layer, int32_t n_req, int32_t total
         p.force_rows = max_new_tokens < 0;
         p.tag = lamps::next_launch_tag();
         LAMPS_HIP(lamps::launch_prefill(p, c->cs));
+        return LAMPS_OK;
+    }
+    LAMPS_CATCH(c)
+}
+
+int lamps_decode_attn_window(lamps_ctx *c, int32_t layer, int32_t batch, int32_t window, int32_t sinks, const void *q,
+                             const int32_t *block_table, const int32_t *ctx_lens, const uint8_t *running_mask, void *out)
+{
+    try {
+        if (!c) return LAMPS_ERR_INVALID;
+        if (!q || !block_table || !ctx_lens || !running_mask || !out)
+            return fail(c, LAMPS_ERR_INVALID, "lamps_decode_attn_window: null argument");
+        if (((uintptr_t)q | (uintptr_t)out) & 15)
+            return fail(c, LAMPS_ERR_INVALID, "lamps_decode_attn_window: q and out must be 16-byte aligned");
+        if (window < 1 || sinks < 0)
+            return fail(c, LAMPS_ERR_INVALID, "lamps_decode_attn_window: window must be 1 or more and sinks 0 or more");
+        if (layer < 0 || layer >= c->cfg.num_layers)
+            return fail(c, LAMPS_ERR_RANGE, "lamps_decode_attn_window: layer out of range");
+        if (batch < 0 || batch > c->cfg.max_batch)
+            return fail(c, LAMPS_ERR_RANGE, "lamps_decode_attn_window: batch out of range");
+        if (batch == 0) return LAMPS_OK;
+        lamps::WindowArgs w = {};
+        fill_decode_args(c, &w.d, layer, batch, q, block_table, ctx_lens, running_mask, out);
+        w.window = window;
+        w.sinks = sinks;
+        LAMPS_HIP(lamps::launch_decode_window(w, c->cs));
+        return LAMPS_OK;
+    }
+    LAMPS_CATCH(c)
+}
+
+int lamps_prefill_attn_window(lamps_ctx *c, int32_t layer, int32_t n_req, int32_t total_tokens, int32_t max_new_tokens,
+                              int32_t window, int32_t sinks, const void *q, const int32_t *q_start,
+                              const int32_t *block_table, const int32_t *ctx_lens, void *out)
+{
+    try {
+        if (!c) return LAMPS_ERR_INVALID;
+        if (!q || !q_start || !block_table || !ctx_lens || !out)
+            return fail(c, LAMPS_ERR_INVALID, "lamps_prefill_attn_window: null argument");
+        if (((uintptr_t)q | (uintptr_t)out) & 15)
+            return fail(c, LAMPS_ERR_INVALID, "lamps_prefill_attn_window: q and out must be 16-byte aligned");
+        if (window < 1 || sinks < 0)
+            return fail(c, LAMPS_ERR_INVALID, "lamps_prefill_attn_window: window must be 1 or more and sinks 0 or more");
+        if (layer < 0 || layer >= c->cfg.num_layers)
+            return fail(c, LAMPS_ERR_RANGE, "lamps_prefill_attn_window: layer out of range");
+        if (n_req < 0 || n_req > c->cfg.max_batch || total_tokens < 0)
+            return fail(c, LAMPS_ERR_RANGE, "lamps_prefill_attn_window: n_req / total_tokens out of range");
+        if (n_req == 0 || total_tokens == 0) return LAMPS_OK;
+        lamps::WindowArgs w = {};
+        fill_decode_args(c, &w.d, layer, n_req, q, block_table, ctx_lens, nullptr, out);
+        w.q_start = q_start;
+        w.window = window;
+        w.sinks = sinks;
+        w.total_tokens = total_tokens;
+        w.max_new_tokens = max_new_tokens > 0 && max_new_tokens < total_tokens ? max_new_tokens : total_tokens;
+        w.force_rows = max_new_tokens < 0;
+        LAMPS_HIP(lamps::launch_prefill_window(w, c->cs));
+        return LAMPS_OK;
+    }
+    LAMPS_CATCH(c)
+}
+
+int lamps_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double original_positions,
+                           double low_turns, double high_turns, double *frequencies)
+{
+    if (!frequencies || rotary_dim < 16 || rotary_dim % 16 != 0) return LAMPS_ERR_INVALID;
+    if (!(base > 1.0) || !std::isfinite(base)) return LAMPS_ERR_INVALID;
+    if (scaling < LAMPS_ROPE_UNSCALED || scaling > LAMPS_ROPE_BY_PARTS) return LAMPS_ERR_INVALID;
+    if (scaling != LAMPS_ROPE_UNSCALED && !(factor >= 1.0 && std::isfinite(factor))) return LAMPS_ERR_INVALID;
+    if (scaling == LAMPS_ROPE_BY_PARTS && (!(original_positions > 0.0) || !(high_turns > low_turns) || !std::isfinite(original_positions) ||
+                                           !std::isfinite(low_turns) || !std::isfinite(high_turns)))
+        return LAMPS_ERR_INVALID;
+    const double n = rotary_dim;
+    if (scaling == LAMPS_ROPE_BASE) base *= std::pow(factor, n / (n - 2));
+    for (int32_t i = 0; i < rotary_dim / 2; ++i) {
+        double f = std::pow(base, -2.0 * i / n);
+        if (scaling == LAMPS_ROPE_LINEAR) {
+            f /= factor;
+        } else if (scaling == LAMPS_ROPE_BY_PARTS) {
+            const double turns = original_positions * f / 6.28318530717958647692;
+            const double g = std::min(1.0, std::max(0.0, (turns - low_turns) / (high_turns - low_turns)));
+            f = g * f + (1.0 - g) * f / factor;
+        }
+        frequencies[i] = f;
+    }
+    return LAMPS_OK;
+}
+
+int lamps_rope_append(lamps_ctx *c, int32_t layer, int32_t batch, const lamps_rope *rope, const void *q, int64_t q_stride,
+                      const void *k_new, int64_t k_stride, const void *v_new, int64_t v_stride, const int32_t *block_table,
+                      int32_t *ctx_lens, const uint8_t *running_mask, int32_t advance, void *q_out)
+{
+    try {
+        if (!c) return LAMPS_ERR_INVALID;
+        lamps::RopeArgs a = {};
+        const char *text = fill_rope_args(c, &a, layer, batch, batch, rope, q, q_stride, k_new, k_stride, v_new, v_stride, block_table, ctx_lens, q_out);
+        if (!text && !running_mask) text = "null argument";
+        if (text) return fail(c, LAMPS_ERR_INVALID, std::string("lamps_rope_append: ") + text);
+        if (layer < 0 || layer >= c->cfg.num_layers)
+            return fail(c, LAMPS_ERR_RANGE, "lamps_rope_append: layer out of range");
+        if (batch < 0 || batch > c->cfg.max_batch)
+            return fail(c, LAMPS_ERR_RANGE, "lamps_rope_append: batch out of range");
+        if (batch == 0) return LAMPS_OK;
+        a.running = running_mask;
+        a.advance = advance != 0;
+        LAMPS_HIP(lamps::launch_rope_append(a, -1, lamps::decode_uses_tiled_layout(a.bf16, a.num_q_heads / a.num_kv_heads), c->cs));
+        return LAMPS_OK;
+    }
+    LAMPS_CATCH(c)
+}
+
+int lamps_rope_append_tokens(lamps_ctx *c, int32_t layer, int32_t n_req, int32_t total_tokens, const lamps_rope *rope,
+                             const void *q, int64_t q_stride, const void *k_new, int64_t k_stride, const void *v_new,
+                             int64_t v_stride, const int32_t *q_start, const int32_t *block_table, const int32_t *ctx_lens,
+                             void *q_out)
+{
+    try {
+        if (!c) return LAMPS_ERR_INVALID;
+        lamps::RopeArgs a = {};
+        const char *text = fill_rope_args(c, &a, layer, n_req, total_tokens, rope, q, q_stride, k_new, k_stride, v_new, v_stride, block_table, ctx_lens, q_out);
+        if (!text && !q_start) text = "null argument";
+        if (text) return fail(c, LAMPS_ERR_INVALID, std::string("lamps_rope_append_tokens: ") + text);
+        if (layer < 0 || layer >= c->cfg.num_layers)
+            return fail(c, LAMPS_ERR_RANGE, "lamps_rope_append_tokens: layer out of range");
+        if (n_req < 0 || n_req > c->cfg.max_batch || total_tokens < 0)
+            return fail(c, LAMPS_ERR_RANGE, "lamps_rope_append_tokens: n_req / total_tokens out of range");
+        if (n_req == 0 || total_tokens == 0) return LAMPS_OK;
+        a.q_start = q_start;
+        LAMPS_HIP(lamps::launch_rope_append(a, total_tokens, lamps::decode_uses_tiled_layout(a.bf16, a.num_q_heads / a.num_kv_heads), c->cs));
+        return LAMPS_OK;
+    }
+    LAMPS_CATCH(c)
+}
+
+int lamps_batch_tables(lamps_ctx *c, int32_t n_req, int32_t total_tokens, const int32_t *cached, const int32_t *new_tokens,
+                       const int32_t *block_ids, int32_t n_ids, int32_t grow, int32_t *block_table, int32_t *ctx_lens,
+                       int32_t *q_start, int64_t *slots, int32_t *report)
+{
+    try {
+        if (!c) return LAMPS_ERR_INVALID;
+        if (!cached || !new_tokens || (n_ids > 0 && !block_ids) || !block_table || !ctx_lens || !q_start)
+            return fail(c, LAMPS_ERR_INVALID, "lamps_batch_tables: null argument");
+        if (n_req < 0 || n_req > c->cfg.max_batch || total_tokens < 0 || n_ids < 0)
+            return fail(c, LAMPS_ERR_RANGE, "lamps_batch_tables: n_req / total_tokens / n_ids out of range");
+        if (n_ids > c->cfg.num_blocks)
+            return fail(c, LAMPS_ERR_RANGE, "lamps_batch_tables: more ids than the pool has blocks");
+        const size_t n = (size_t)n_req;
+        const struct { const void *p; size_t bytes; } in[] = {{cached, n * 4}, {new_tokens, n * 4}, {block_ids, (size_t)n_ids * 4}},
+            out[] = {{block_table, n * c->cfg.max_blocks_per_req * 4}, {ctx_lens, n * 4}, {q_start, (n + 1) * 4},
+                     {slots, (size_t)total_tokens * 8}, {report, 16}};
+        for (int i = 0; i < 5; ++i) {
+            for (int j = 0; j < 3; ++j)
+                if (overlap(out[i].p, out[i].bytes, in[j].p, in[j].bytes))
+                    return fail(c, LAMPS_ERR_INVALID, "lamps_batch_tables: an output overlaps an input");
+            for (int j = 0; j < i; ++j)
+                if (overlap(out[i].p, out[i].bytes, out[j].p, out[j].bytes))
+                    return fail(c, LAMPS_ERR_INVALID, "lamps_batch_tables: two outputs overlap");
+        }
+        lamps::TableArgs a = {};
+        a.cached = cached;
+        a.new_tokens = new_tokens;
+        a.block_ids = block_ids;
+        a.block_table = block_table;
+        a.ctx_lens = ctx_lens;
+        a.q_start = q_start;
+        a.report = report;
+        a.slots = slots;
+        a.n_req = n_req;
+        a.total_tokens = total_tokens;
+        a.n_ids = n_ids;
+        a.grow = grow != 0;
+        a.max_blocks = c->cfg.max_blocks_per_req;
+        a.num_blocks = c->cfg.num_blocks;
+        a.log2_block_size = c->d.log2_bs;
+        LAMPS_HIP(lamps::launch_batch_tables(a, c->cs));
         return LAMPS_OK;
     }
     LAMPS_CATCH(c)

@@ -1,0 +1,225 @@
+"""GPU parity of lamps_decode_attn_window and lamps_prefill_attn_window: every new token over the last positions up to its own and
+the first few, against plain numpy in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import lamps_workloads as W
+from operator_forms import f64, seen, window_attn
+from rig import Rig, n2t, to_f64
+
+pytestmark = pytest.mark.gpu
+
+#        dtype  H  Hkv D    bs  (context, new tokens) per request                    windows and sinks
+CASES = [
+    ("bf16", 8, 2, 128, 16, [(130, 130), (47, 5), (16, 16), (1, 1), (200, 64), (33, 0)], [(1, 0), (16, 4), (50, 17), (129, 3), (1000, 0)]),
+    ("bf16", 4, 4, 128, 16, [(130, 130), (47, 5), (16, 16), (1, 1), (95, 31)], [(1, 1), (15, 0), (40, 16), (500, 7)]),
+    ("bf16", 8, 2, 64, 32, [(95, 95), (64, 33), (300, 2)], [(7, 5), (64, 40)]),
+    ("bf16", 3, 3, 64, 64, [(150, 150), (400, 20)], [(33, 1), (100, 70)]),
+    ("bf16", 16, 1, 256, 16, [(70, 70), (131, 2)], [(20, 2), (65, 33)]),
+    ("bf16", 4, 4, 256, 32, [(90, 90), (50, 6)], [(31, 4)]),
+    ("bf16", 6, 2, 128, 16, [(100, 100), (77, 10)], [(32, 0)]),                    # groups of 3
+    ("bf16", 32, 1, 128, 16, [(45, 45), (90, 3)], [(17, 3)]),                      # 32 heads per kv head
+    ("bf16", 40, 1, 64, 16, [(40, 40)], [(9, 2)]),                                 # 40
+    ("bf16", 8, 2, 128, 16, [(700, 700), (1200, 37)], [(260, 4), (97, 70)]),       # several tiles of new tokens
+    ("bf16", 4, 4, 128, 16, [(700, 700), (1200, 37)], [(260, 4)]),
+    ("bf16", 8, 4, 64, 16, [(900, 30), (700, 1), (1500, 100)], [(512, 16)]),
+    ("f32", 4, 4, 64, 16, [(40, 40), (117, 3), (64, 1), (9, 0), (33, 33)], [(1, 0), (13, 3), (30, 20), (200, 5)]),
+    ("f32", 8, 2, 32, 16, [(150, 150), (80, 7)], [(11, 2), (64, 16)]),
+    ("f32", 8, 2, 128, 32, [(130, 130), (300, 9)], [(50, 4)]),
+    ("f32", 3, 1, 64, 64, [(170, 100)], [(33, 4)]),                                # groups of 3
+]
+# Half a step of bf16 (2^-8 of the value): once for the output, and where the weights are rounded to it, once for each of them and their
+# sum.  On top the sums in 32 bits.  A score is a sum of D products: at most 12 roundings deep, of |q||k| scale < 30 for normal vectors, so off
+# by 12 2^-24 30 = 2e-5, which is the relative error of a weight; values of the pair (high part and remainder) are off by 2^-17 = 8e-6.
+STEP = 2.0 ** -8
+ACC = 6e-5
+
+
+def bound(dtype, out, size, rounded):
+    if dtype == "f32":
+        return ACC * (size + np.abs(out)) + 1e-6
+    return STEP * np.abs(out) + (STEP * (size + np.abs(out)) if rounded else 0.0) + ACC * (size + np.abs(out)) + 1e-6
+
+
+def _setup(dtype, H, Hkv, D, bs, reqs, window, sinks, seed, layers=2, clean=True):
+    """Pools in which what no new token sees is NaN, and table entries of blocks of nothing else name no block."""
+    ctx = [c for c, _ in reqs]
+    geom = W.Geometry(layers, H, Hkv, D, bs, sum((c + bs - 1) // bs for c in ctx) + 4, max((c + bs - 1) // bs for c in ctx) + 1, dtype)
+    rig = Rig(geom, len(reqs))
+    table, _ = W.deal_block_table(W.permutation(seed, geom.num_blocks), ctx, geom)
+    K, V = zip(*[W.logical_kv(seed + 17 * r, geom, c) for r, c in enumerate(ctx)])
+    KN, VN = [k.copy() for k in K], [v.copy() for v in V]
+    holes = table.copy()
+    for r, (c, n) in enumerate(reqs):
+        any_sees = np.zeros(c, dtype=bool)
+        for p in range(c - max(n, 1), c):
+            any_sees |= seen(p, c, window, sinks)
+        if clean:
+            nan = np.uint16(0x7FC0) if dtype == "bf16" else np.float32("nan")
+            KN[r][~any_sees], VN[r][~any_sees] = nan, nan
+            for b in range((c + bs - 1) // bs):
+                if not any_sees[b * bs:(b + 1) * bs].any():
+                    holes[r, b] = -7
+    rig.page_requests(layers - 1, table, KN, VN)
+    return geom, rig, holes, K, V, ctx
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,D,bs,reqs,looks", CASES)
+def test_decode(dtype, H, Hkv, D, bs, reqs, looks):
+    for w, (window, sinks) in enumerate(looks):
+        one = [(c, 1) for c, _ in reqs] + [(0, 0)]
+        geom, rig, table, K, V, ctx = _setup(dtype, H, Hkv, D, bs, one, window, sinks, 31 + D + w)
+        B = len(ctx)
+        q = W.queries(5 + w, geom, B)
+        running = np.ones(B, dtype=np.uint8)
+        running[1:2] = 0
+        dev = rig.dev
+        out = torch.full((B, H, D), 2.5, dtype=rig.tdtype, device=dev)
+        args = n2t(q, dev), torch.as_tensor(table, device=dev), torch.tensor(ctx, dtype=torch.int32, device=dev), torch.as_tensor(running, device=dev)
+        torch.cuda.synchronize()
+        rig.lamps.decode_attn_window(1, B, window, sinks, *args, out)
+        again = torch.full_like(out, 2.5)
+        torch.cuda.synchronize()
+        rig.lamps.decode_attn_window(1, B, window, sinks, *args, again)
+        torch.cuda.synchronize()
+        assert torch.equal(out, again)
+        got = to_f64(out)
+        for r in range(B):
+            if not running[r]:
+                assert (got[r] == 2.5).all()
+            elif ctx[r] == 0:
+                assert (got[r] == 0).all()
+            else:
+                ref, size = window_attn(f64(q[r:r + 1]), f64(K[r]), f64(V[r]), ctx[r] - 1, window, sinks)
+                off = np.abs(got[r] - ref[0]) - bound(dtype, ref[0], size[0], False)
+                assert (off <= 0).all(), (window, sinks, r, ctx[r], off.max())
+        rig.close()
+
+
+def _prefill(rig, layer, q, reqs, table, window, sinks, out, most):
+    dev = rig.dev
+    start = np.concatenate([[0], np.cumsum([n for _, n in reqs])])
+    args = torch.tensor(start, dtype=torch.int32, device=dev), torch.as_tensor(table, device=dev), \
+        torch.tensor([c for c, _ in reqs], dtype=torch.int32, device=dev)
+    qd = q if torch.is_tensor(q) else n2t(q, dev)
+    torch.cuda.synchronize()
+    rig.lamps.prefill_attn_window(layer, len(reqs), qd.shape[0], window, sinks, qd, *args, out, max_new_tokens=most)
+    torch.cuda.synchronize()
+    return start
+
+
+@pytest.mark.parametrize("rows", [False, True])
+@pytest.mark.parametrize("dtype,H,Hkv,D,bs,reqs,looks", CASES)
+def test_prefill(dtype, H, Hkv, D, bs, reqs, looks, rows):
+    """Rows behind the last request's are left as they were."""
+    for w, (window, sinks) in enumerate(looks):
+        geom, rig, table, K, V, ctx = _setup(dtype, H, Hkv, D, bs, reqs, window, sinks, 77 + D + w)
+        total = sum(n for _, n in reqs)
+        q = W.queries(9 + w, geom, total + 3)
+        out = torch.full((total + 3, H, D), 2.5, dtype=rig.tdtype, device=rig.dev)
+        again = out.clone()
+        most = -1 if rows else (max(n for _, n in reqs) if w % 2 else 0)
+        start = _prefill(rig, 1, q, reqs, table, window, sinks, out, most)
+        _prefill(rig, 1, q, reqs, table, window, sinks, again, most)
+        assert torch.equal(out, again)
+        got = to_f64(out)
+        assert (got[total:] == 2.5).all()
+        for r, (c, n) in enumerate(reqs):
+            if n:
+                ref, size = window_attn(f64(q[start[r]:start[r + 1]]), f64(K[r]), f64(V[r]), c - n, window, sinks)
+                off = np.abs(got[start[r]:start[r + 1]] - ref) - bound(dtype, ref, size, not rows)
+                assert (off <= 0).all(), (window, sinks, r, c, n, off.max())
+        rig.close()
+
+
+@pytest.mark.parametrize("what", ["nan", "inf"])
+@pytest.mark.parametrize("dtype,H,Hkv,D,bs", [("bf16", 8, 2, 128, 16), ("bf16", 4, 4, 128, 16), ("bf16", 8, 2, 64, 16), ("bf16", 4, 4, 64, 16),
+                                              ("bf16", 8, 1, 256, 16), ("bf16", 2, 2, 256, 16), ("f32", 4, 2, 64, 16), ("f32", 4, 4, 128, 16),
+                                              ("f32", 4, 1, 32, 16)])
+def test_what_a_token_does_not_see_has_no_part_in_its_row(dtype, H, Hkv, D, bs, what):
+    """Keys and values that are no finite numbers, at one position: the rows that see it are no finite numbers, all others as without."""
+    reqs, window, sinks, at = [(150, 150), (90, 20)], 40, 3, (60, 75)
+    geom, rig, table, K, V, ctx = _setup(dtype, H, Hkv, D, bs, reqs, window, sinks, 3, clean=False)
+    total = sum(n for _, n in reqs)
+    q = W.queries(4, geom, total)
+    bad = {"nan": (0x7FC0, np.nan), "inf": (0x7F80, np.inf)}[what][0 if dtype == "bf16" else 1]
+    for keys in (True, False):
+        for rows in (0, -1):
+            rig.page_requests(1, table, K, V)
+            clean = torch.zeros((total, H, D), dtype=rig.tdtype, device=rig.dev)
+            _prefill(rig, 1, q, reqs, table, window, sinks, clean, rows)
+            Kb, Vb = [k.copy() for k in K], [v.copy() for v in V]
+            for r, p in enumerate(at):
+                (Kb if keys else Vb)[r][p] = bad
+            rig.page_requests(1, table, Kb, Vb)
+            out = torch.zeros_like(clean)
+            start = _prefill(rig, 1, q, reqs, table, window, sinks, out, rows)
+            for r, (c, n) in enumerate(reqs):
+                sees = np.array([seen(p, c, window, sinks)[at[r]] for p in range(c - n, c)])
+                a, b = clean[start[r]:start[r + 1]].cpu(), out[start[r]:start[r + 1]].cpu()
+                assert torch.equal(a[~sees], b[~sees]), (keys, rows, r)
+                if what == "nan" or not keys:             # (an infinite key may give weights of 0)
+                    assert not torch.isfinite(b[sees]).any(), (keys, rows, r)
+    rig.close()
+
+
+def test_a_full_window_is_the_whole_attention():
+    for dtype, H, Hkv, D in [("bf16", 8, 2, 128), ("bf16", 4, 4, 64), ("f32", 4, 2, 64)]:
+        reqs = [(300, 300), (77, 1)]
+        geom, rig, table, K, V, ctx = _setup(dtype, H, Hkv, D, 16, reqs, 1 << 30, 0, 8)
+        total = sum(n for _, n in reqs)
+        q = n2t(W.queries(1, geom, total), rig.dev)
+        outs = [torch.zeros((total, H, D), dtype=rig.tdtype, device=rig.dev) for _ in range(2)]
+        start = _prefill(rig, 1, q, reqs, table, 2 ** 31 - 1, 2 ** 31 - 1, outs[0], 0)
+        rig.lamps.prefill_attn(1, 2, total, q, torch.tensor(start, dtype=torch.int32, device=rig.dev), torch.as_tensor(table, device=rig.dev),
+                               torch.tensor(ctx, dtype=torch.int32, device=rig.dev), outs[1])
+        torch.cuda.synchronize()
+        a, b = to_f64(outs[0]), to_f64(outs[1])
+        for r, (c, n) in enumerate(reqs):
+            at = slice(start[r], start[r + 1])
+            ref, size = window_attn(f64(W.queries(1, geom, total)[at]), f64(K[r]), f64(V[r]), c - n, 1 << 30, 0)
+            assert (np.abs(a[at] - b[at]) <= 2 * bound(dtype, ref, size, True)).all()
+        rig.close()
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,D,bs,layers,batch", [("bf16", 8, 2, 128, 16, 1, 1), ("bf16", 4, 4, 128, 16, 3, 3), ("f32", 8, 2, 64, 32, 1, 2)])
+def test_long_contexts_in_parts(dtype, H, Hkv, D, bs, layers, batch):
+    """Few ranges of wide windows, which workgroups share."""
+    window, sinks = 2000, 33
+    reqs = [(5000 - 700 * r, 1) for r in range(batch)]
+    geom, rig, table, K, V, ctx = _setup(dtype, H, Hkv, D, bs, reqs, window, sinks, 91, layers=layers)
+    q = W.queries(2, geom, batch)
+    out = torch.zeros((batch, H, D), dtype=rig.tdtype, device=rig.dev)
+    rig.lamps.decode_attn_window(layers - 1, batch, window, sinks, n2t(q, rig.dev), torch.as_tensor(table, device=rig.dev),
+                                 torch.tensor(ctx, dtype=torch.int32, device=rig.dev), torch.ones(batch, dtype=torch.uint8, device=rig.dev), out)
+    torch.cuda.synchronize()
+    for r in range(batch):
+        ref, size = window_attn(f64(q[r:r + 1]), f64(K[r]), f64(V[r]), ctx[r] - 1, window, sinks)
+        assert (np.abs(to_f64(out)[r] - ref[0]) <= bound(dtype, ref[0], size[0], False)).all()
+    rig.close()
+
+
+def test_bad_lengths_and_entries_are_harmless():
+    """A context longer than its row is clamped (decode) or ignored (many tokens), one shorter than its new tokens ignored; a row whose
+    entries name no block of the pool is written with something, the others are as without it."""
+    for dtype, H, Hkv, D in [("bf16", 8, 2, 128), ("bf16", 4, 4, 64), ("f32", 4, 2, 32)]:
+        reqs = [(70, 70), (60, 30), (50, 50)]
+        geom, rig, table, K, V, ctx = _setup(dtype, H, Hkv, D, 16, reqs, 40, 2, 8)
+        total = sum(n for _, n in reqs)
+        q = W.queries(1, geom, total)
+        good = torch.full((total, H, D), 2.5, dtype=rig.tdtype, device=rig.dev)
+        start = _prefill(rig, 1, q, reqs, table, 40, 2, good, 0)
+        for lens in ([70, 100000, 50], [70, 29, 50]):
+            out = torch.full_like(good, 2.5)
+            rig.lamps.prefill_attn_window(1, 3, total, 40, 2, n2t(q, rig.dev), torch.tensor(start, dtype=torch.int32, device=rig.dev),
+                                          torch.as_tensor(table, device=rig.dev), torch.tensor(lens, dtype=torch.int32, device=rig.dev), out)
+            torch.cuda.synchronize()
+            assert (out[start[1]:start[2]] == 2.5).all()
+            assert torch.equal(out[:start[1]], good[:start[1]]) and torch.equal(out[start[2]:], good[start[2]:])
+        wild = table.copy()
+        wild[1] = geom.num_blocks + 5
+        out = torch.full_like(good, 2.5)
+        _prefill(rig, 1, q, reqs, wild, 40, 2, out, 0)
+        assert torch.equal(out[:start[1]], good[:start[1]]) and torch.equal(out[start[2]:], good[start[2]:])
+        rig.close()
