@@ -101,7 +101,7 @@ struct WindowArgs {
     const int32_t *q_start;      // [batch + 1]; nullptr: one new token per request, the last of its context
     int32_t window, sinks;
     int32_t total_tokens, max_new_tokens, force_rows;   // as in PrefillArgs
-    int32_t parts;               // workgroups that share a range (filled in by the launcher)
+    int32_t parts, items;        // workgroups that share a range or tile; tiles of a head (filled in by the launcher)
 };
 hipError_t launch_decode_window(const WindowArgs &a, hipStream_t stream);
 hipError_t launch_prefill_window(const WindowArgs &a, hipStream_t stream);

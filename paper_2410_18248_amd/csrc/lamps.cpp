@@ -903,8 +903,8 @@ int lamps_decode_attn_window(lamps_ctx *c, int32_t layer, int32_t batch, int32_t
         if (batch == 0) return LAMPS_OK;
         lamps::WindowArgs w = {};
         fill_decode_args(c, &w.d, layer, batch, q, block_table, ctx_lens, running_mask, out);
-        w.window = window;
-        w.sinks = sinks;
+        w.window = std::min(window, 1 << 30);             // (no row has more positions)
+        w.sinks = std::min(sinks, 1 << 30);
         LAMPS_HIP(lamps::launch_decode_window(w, c->cs));
         return LAMPS_OK;
     }
@@ -931,8 +931,8 @@ int lamps_prefill_attn_window(lamps_ctx *c, int32_t layer, int32_t n_req, int32_
         lamps::WindowArgs w = {};
         fill_decode_args(c, &w.d, layer, n_req, q, block_table, ctx_lens, nullptr, out);
         w.q_start = q_start;
-        w.window = window;
-        w.sinks = sinks;
+        w.window = std::min(window, 1 << 30);             // (no row has more positions)
+        w.sinks = std::min(sinks, 1 << 30);
         w.total_tokens = total_tokens;
         w.max_new_tokens = max_new_tokens > 0 && max_new_tokens < total_tokens ? max_new_tokens : total_tokens;
         w.force_rows = max_new_tokens < 0;

@@ -13,6 +13,7 @@
 #include "attn_reducers.h"
 #include "internal.h"
 #include "requests.h"
+#include "tile_parts.h"
 
 namespace lamps {
 namespace {
@@ -27,10 +28,12 @@ struct Sight {
     int end, lo, sinks;                  // sees t < end if t >= lo or t < sinks; lo = 0 where the two stretches meet
     int first, start, units;             // units of sinks; position of the first unit behind them; all units
 
-    __device__ __forceinline__ Sight(int C, int window, int want)
+    __device__ __forceinline__ Sight(int C, int window, int want) : Sight(max(C, 0), max(0, max(C, 0) - window), want, std::true_type{}) {}
+    // (of several tokens together: `from` the first one's, C the last one's)
+    __device__ __forceinline__ Sight(int C, int from, int want, std::true_type)
     {
-        end = max(C, 0);
-        lo = max(0, end - window);
+        end = C;
+        lo = from;
         sinks = min(want, lo);
         if (lo <= sinks) lo = sinks = 0;
         first = (sinks + U - 1) / U;
@@ -431,6 +434,8 @@ __global__ __launch_bounds__(kThreads) void window_rows(const WindowArgs w)
     });
 }
 
+#include "window_tiles.h"
+
 // ---------------------------------------------------------------- launches
 
 // Positions that the sight of one token can have: of `span` tokens together so many more.
@@ -471,6 +476,45 @@ hipError_t launch_one(WindowArgs w, hipStream_t s)
     if (e != hipSuccess || w.parts == 1) return e;
     hipLaunchKernelGGL(window_merge<R::kBF16>, dim3((unsigned)ranges, (unsigned)((a.heads_per_pass * a.head_dim + 127) / 128)), dim3(64 * kMergeWaves), 0, s, w);
     return hipGetLastError();
+}
+
+template <int D, bool TILED, int kCB>
+hipError_t launch_tiles(WindowArgs w, hipStream_t s)
+{
+    const DecodeArgs &a = w.d;
+    const int WT = kWaves * (16 * kCB / (a.num_q_heads / a.num_kv_heads));
+    const long long items = (long long)w.total_tokens / WT + a.batch, tiles = items * a.num_kv_heads;
+    const long long stages = (std::min((long long)a.max_blocks * a.block_size, (long long)w.window + w.sinks + WT) + 31) / 32 + 1;
+    const long long state = (long long)tile_state_floats(D, kWaves * 16 * kCB) * (long long)sizeof(float);
+    // two workgroups fit a CU; four stages at least to a part
+    long long parts = std::min(512 / tiles, stages / 4);
+    parts = std::max(1LL, std::min(parts, (long long)a.partial_capacity / (state * tiles)));
+    const long long grid = (tiles * parts + 7) / 8 * 8, join = (tiles + 7) / 8 * 8;
+    if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
+    w.items = (int)items;
+    w.parts = (int)parts;
+    if (parts == 1) {
+        hipLaunchKernelGGL((window_tiles<D, TILED, kCB, false>), dim3((unsigned)grid), dim3(kThreads), 0, s, w);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((window_tiles<D, TILED, kCB, true>), dim3((unsigned)grid), dim3(kThreads), 0, s, w);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((window_join<D, kCB>), dim3((unsigned)join, kWaves * kCB), dim3(kThreads), 0, s, w);
+    return hipGetLastError();
+}
+
+template <int D, bool TILED>
+hipError_t launch_tiles(const WindowArgs &w, hipStream_t s)
+{
+    const int G = w.d.num_q_heads / w.d.num_kv_heads;
+    if constexpr (D >= 256) {                         // (32 columns to a wave are more than 256 registers)
+        if constexpr (TILED)
+            if (G > 16) return launch_tiles<D, TILED, 2>(w, s);
+        return launch_tiles<D, TILED, 1>(w, s);
+    } else {
+        return G > 16 || (long long)w.max_new_tokens * G > 512 ? launch_tiles<D, TILED, 2>(w, s) : launch_tiles<D, TILED, 1>(w, s);
+    }
 }
 
 template <int LPT>
@@ -514,7 +558,17 @@ hipError_t launch_decode_window(const WindowArgs &w, hipStream_t stream)
 
 hipError_t launch_prefill_window(const WindowArgs &w, hipStream_t stream)
 {
-    if (w.d.batch == 0 || w.total_tokens == 0) return hipSuccess;
+    const DecodeArgs &a = w.d;
+    if (a.batch == 0 || w.total_tokens == 0) return hipSuccess;
+    const int G = a.num_q_heads / a.num_kv_heads;
+    // (the kernels of tiles keep the distance between two blocks of a pool in 32 bits)
+    const unsigned long long stride = 2ull * a.num_layers * a.num_kv_heads * a.block_size * a.head_dim;
+    if (a.bf16 && G <= 32 && !w.force_rows && stride <= 0xffffffffull) {
+        const bool tiled = decode_uses_tiled_layout(a.bf16, G);
+        if (a.head_dim == 64) return tiled ? launch_tiles<64, true>(w, stream) : launch_tiles<64, false>(w, stream);
+        if (a.head_dim == 128) return tiled ? launch_tiles<128, true>(w, stream) : launch_tiles<128, false>(w, stream);
+        if (a.head_dim == 256) return tiled ? launch_tiles<256, true>(w, stream) : launch_tiles<256, false>(w, stream);
+    }
     return launch_window(w, stream);
 }
 
