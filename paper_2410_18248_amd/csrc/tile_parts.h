@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace lamps {
 namespace {
 
@@ -13,6 +15,31 @@ typedef __attribute__((address_space(4))) const int32_t *table_ptr;   // read-on
 
 // s_waitcnt immediate: wait until at most n of the wave's vector memory operations are outstanding
 constexpr int vmcnt(int n) { return 0x0F70 | (n & 15) | (n >> 4) << 14; }
+
+// The positions that one token sees, in aligned units of U: those of the sinks, then those of the window.
+template <int U>
+struct Sight {
+    int end, lo, sinks;                  // sees t < end if t >= lo or t < sinks; lo = 0 where the two stretches meet
+    int first, start, units;             // units of sinks; position of the first unit behind them; all units
+
+    __device__ __forceinline__ Sight(int C, int window, int want) : Sight(max(C, 0), max(0, max(C, 0) - window), want, std::true_type{}) {}
+    // (of several tokens together: `from` the first one's, C the last one's)
+    __device__ __forceinline__ Sight(int C, int from, int want, std::true_type)
+    {
+        end = C;
+        lo = from;
+        sinks = min(want, lo);
+        if (lo <= sinks) lo = sinks = 0;
+        first = (sinks + U - 1) / U;
+        start = max(lo / U, first) * U;
+        units = first + (max(end - start, 0) + U - 1) / U;
+    }
+    __device__ __forceinline__ int at(int u) const { return u < first ? u * U : start + (u - first) * U; }
+    __device__ __forceinline__ int unit_of(int t) const { return t < start ? t / U : first + (t - start) / U; }   // of a position that lies in one
+    // (no branches: see window_attn.hip)
+    __device__ __forceinline__ bool sees(int t) const { return (t < end) & ((t >= lo) | (t < sinks)); }
+    __device__ __forceinline__ bool sees_all(int t) const { return (t + U <= end) & ((t >= lo) | (t + U <= sinks)); }   // of the unit at t
+};
 
 // Stores a column's N slabs of 16 outputs, those of quarter qd being 4 qd .. of each.  Odd and even quarters exchange halves of
 // two slabs, so that a lane stores 16 bytes and an instruction 64 of a row: by 8 and 32, 24 prompts of 16 to 700 tokens on 40 heads took

@@ -15,36 +15,24 @@
 #include "requests.h"
 #include "tile_parts.h"
 
+#ifndef WTEAM
+#define WTEAM 256
+#endif
+#ifndef WPT
+#define WPT 512
+#endif
+#ifndef WPS
+#define WPS 4
+#endif
+#ifndef WCB
+#define WCB 512
+#endif
 namespace lamps {
 namespace {
 
 // ---------------------------------------------------------------- what a token sees
 
 constexpr float kLeast = -FLT_MAX;       // a reference below which no finite score lies
-
-// The positions that one token sees, in aligned units of U: those of the sinks, then those of the window.
-template <int U>
-struct Sight {
-    int end, lo, sinks;                  // sees t < end if t >= lo or t < sinks; lo = 0 where the two stretches meet
-    int first, start, units;             // units of sinks; position of the first unit behind them; all units
-
-    __device__ __forceinline__ Sight(int C, int window, int want) : Sight(max(C, 0), max(0, max(C, 0) - window), want, std::true_type{}) {}
-    // (of several tokens together: `from` the first one's, C the last one's)
-    __device__ __forceinline__ Sight(int C, int from, int want, std::true_type)
-    {
-        end = C;
-        lo = from;
-        sinks = min(want, lo);
-        if (lo <= sinks) lo = sinks = 0;
-        first = (sinks + U - 1) / U;
-        start = max(lo / U, first) * U;
-        units = first + (max(end - start, 0) + U - 1) / U;
-    }
-    __device__ __forceinline__ int at(int u) const { return u < first ? u * U : start + (u - first) * U; }
-    // (no branches: see consume() below)
-    __device__ __forceinline__ bool sees(int t) const { return (t < end) & ((t >= lo) | (t < sinks)); }
-    __device__ __forceinline__ bool sees_all(int t) const { return (t + U <= end) & ((t >= lo) | (t + U <= sinks)); }   // of the unit at t
-};
 
 // A state without a position is (kLeast, 0, 0).  A row of no positions is zero; one whose weights are not numbers is none either.
 __device__ __forceinline__ float reciprocal(float L, bool none) { return none ? 0.0f : 1.0f / L; }
@@ -487,8 +475,10 @@ hipError_t launch_tiles(WindowArgs w, hipStream_t s)
     const long long stages = (std::min((long long)a.max_blocks * a.block_size, (long long)w.window + w.sinks + WT) + 31) / 32 + 1;
     const long long state = (long long)tile_state_floats(D, kWaves * 16 * kCB) * (long long)sizeof(float);
     // two workgroups fit a CU; four stages at least to a part
-    long long parts = std::min(512 / tiles, stages / 4);
-    parts = std::max(1LL, std::min(parts, (long long)a.partial_capacity / (state * tiles)));
+    // (about as many tiles as there are: half of the requests' last ones are there besides the full ones)
+    const long long there = std::max(1LL, ((long long)w.total_tokens / WT + a.batch / 2) * a.num_kv_heads);
+    long long parts = std::min(WPT / there, stages / WPS);
+    parts = std::max(1LL, std::min({parts, (long long)kMostParts, (long long)a.partial_capacity / (state * tiles)}));
     const long long grid = (tiles * parts + 7) / 8 * 8, join = (tiles + 7) / 8 * 8;
     if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
     w.items = (int)items;
@@ -500,7 +490,22 @@ hipError_t launch_tiles(WindowArgs w, hipStream_t s)
     hipLaunchKernelGGL((window_tiles<D, TILED, kCB, true>), dim3((unsigned)grid), dim3(kThreads), 0, s, w);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((window_join<D, kCB>), dim3((unsigned)join, kWaves * kCB), dim3(kThreads), 0, s, w);
+    if (parts <= 4)
+        hipLaunchKernelGGL((window_join<D, kCB, true>), dim3((unsigned)join, kWaves * kCB, (D + 127) / 128), dim3(kThreads), 0, s, w);
+    else
+        hipLaunchKernelGGL((window_join<D, kCB, false>), dim3((unsigned)join, kWaves * kCB, D / 32), dim3(kThreads), 0, s, w);
+    return hipGetLastError();
+}
+
+template <int D, bool TILED, int kCB>
+hipError_t launch_teams(WindowArgs w, hipStream_t s)
+{
+    const int WT = 8 * (16 * kCB / (w.d.num_q_heads / w.d.num_kv_heads));
+    const long long items = (long long)w.total_tokens / WT + w.d.batch, grid = (items * w.d.num_kv_heads + 7) / 8 * 8;
+    if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
+    w.items = (int)items;
+    w.parts = 1;
+    hipLaunchKernelGGL((window_teams<D, TILED, kCB>), dim3((unsigned)grid), dim3(512), 128 << 10, s, w);
     return hipGetLastError();
 }
 
@@ -508,12 +513,14 @@ template <int D, bool TILED>
 hipError_t launch_tiles(const WindowArgs &w, hipStream_t s)
 {
     const int G = w.d.num_q_heads / w.d.num_kv_heads;
-    if constexpr (D >= 256) {                         // (32 columns to a wave are more than 256 registers)
-        if constexpr (TILED)
-            if (G > 16) return launch_tiles<D, TILED, 2>(w, s);
-        return launch_tiles<D, TILED, 1>(w, s);
+    if constexpr (D == 128) {
+        const int WT = 256 / G;
+        if (w.d.scale_log2e > 0.0f && w.d.num_kv_heads * ((long long)w.total_tokens / WT) >= WTEAM) return launch_teams<D, TILED, 2>(w, s);
+    }
+    if constexpr (D >= 256) {                         // (as in prefill_mfma)
+        return launch_tiles<D, TILED, TILED ? 2 : 1>(w, s);
     } else {
-        return G > 16 || (long long)w.max_new_tokens * G > 512 ? launch_tiles<D, TILED, 2>(w, s) : launch_tiles<D, TILED, 1>(w, s);
+        return G > 16 || (long long)w.max_new_tokens * G > WCB ? launch_tiles<D, TILED, 2>(w, s) : launch_tiles<D, TILED, 1>(w, s);
     }
 }
 

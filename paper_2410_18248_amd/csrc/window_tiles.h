@@ -16,13 +16,19 @@
 struct TileAt {
     int r, g, tile, first, n_new, ctx, part, item;
 };
-template <int THREADS>
+// The number of a workgroup's item, part by part; < 0: none.
+__device__ __forceinline__ int tile_item(const WindowArgs &w, unsigned block)
+{
+    const unsigned all = (unsigned)w.items * (unsigned)w.d.num_kv_heads * (unsigned)w.parts, per = (all + 7) / 8, i = (block & 7) * per + (block >> 3);
+    return block >> 3 < per && i < all ? (int)i : -1;
+}
 __device__ __forceinline__ bool tile_at(const WindowArgs &w, int WT, TileAt &at)
 {
     const DecodeArgs &a = w.d;
-    const unsigned items = (unsigned)w.items, all = items * (unsigned)a.num_kv_heads * (unsigned)w.parts, per = (all + 7) / 8;
-    unsigned i = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if ((blockIdx.x >> 3) >= per || i >= all) return false;
+    const unsigned items = (unsigned)w.items;
+    const int i0 = tile_item(w, blockIdx.x);
+    if (i0 < 0) return false;
+    const unsigned i = (unsigned)i0;
     // (uniform, and said to be: divisions go through the vector ALUs, and addresses of loads into LDS are scalars)
     const unsigned run = (unsigned)__builtin_amdgcn_readfirstlane((int)(i / (unsigned)w.parts));
     at.part = (int)(i - run * (unsigned)w.parts);
@@ -42,25 +48,37 @@ __device__ __forceinline__ bool tile_at(const WindowArgs &w, int WT, TileAt &at)
 
 constexpr size_t tile_state_floats(int D, int columns) { return (size_t)columns * (D + 2); }
 
-// The kernels that keep to 256 registers: two workgroups to a CU.
-template <int D, int kCB>
-constexpr int tile_groups() { return D <= 128 ? 2 : 1; }   // stages per barrier: two where they fit
+// Narrow tiles, of 64 columns: one stage per barrier, operands read one after the other, for three or four workgroups to a CU.
+#ifndef SMALLN
+#define SMALLN 1
+#endif
+#ifndef SMALLS
+#define SMALLS 0
+#endif
+template <int D, int kCB, bool SPLIT>
+constexpr bool tile_small() { return D <= 128 && kCB == 1 && (SPLIT ? SMALLS : SMALLN); }
+// Stages per barrier, and groups of them that LDS holds.
+template <int D, int kCB, bool SPLIT>
+constexpr int tile_groups() { return D <= 128 && kCB > 1 ? 2 : 1; }
+template <int D, int kCB, bool SPLIT>
+constexpr int tile_buffers() { return D <= 128 && SPLIT && kCB == 1 && !tile_small<D, kCB, SPLIT>() ? 4 : 2; }
 
 template <int D, bool TILED, int kCB, bool SPLIT>
-__global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void window_tiles(const WindowArgs w)
+__global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : (tile_small<D, kCB, SPLIT>()) ? (D == 128 && TILED ? 3 : 4) : 2) void window_tiles(const WindowArgs w)
 {
-    constexpr int kCols = 16 * kCB, GRP = tile_groups<D, kCB>(), NB = 2;
+    constexpr int kCols = 16 * kCB, GRP = tile_groups<D, kCB, SPLIT>(), NB = tile_buffers<D, kCB, SPLIT>();
     constexpr int NK = D / 32, NS = D / 16, U = D * 2, NU = D / 8;
     constexpr int LPT = (2 * U) / kThreads;           // 16-byte units per thread, pool and stage
     constexpr int SUBB = 16 * D * 2, VOFF = 2 * SUBB, STAGE = 4 * SUBB, GSTAGE = GRP * STAGE;
-    constexpr bool kLean = D >= 256;                  // operands are read one after the other: registers
+    constexpr bool kLean = D >= 256 || (D == 128 && tile_small<D, kCB, SPLIT>());   // operands are read one after the other: registers
+    constexpr int kLoads = GRP * 2 * LPT;             // of a group, of one wave; all groups have as many
     static_assert(NB * GSTAGE <= 65536 && LPT >= 1 && (2 * U) % kThreads == 0, "head_dim");
     __shared__ __align__(16) char lds[NB * GSTAGE];
 
     const DecodeArgs &a = w.d;
     const int G = a.num_q_heads / a.num_kv_heads, TW = kCols / G, WT = kWaves * TW;
     TileAt at;
-    if (!tile_at<kThreads>(w, WT, at)) return;
+    if (!tile_at(w, WT, at)) return;
     const int r = at.r, g = at.g, first = at.first, base_pos = at.ctx - at.n_new;
     const int n_new = min(at.n_new, w.total_tokens - first);
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -81,7 +99,13 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void window_
     const bool none = wave_tok >= n_new;
     const int wave_min = __builtin_amdgcn_readfirstlane(none ? 0x3fffffff : base_pos + wave_tok);
     const int wave_max = __builtin_amdgcn_readfirstlane(none ? -1 : base_pos + min(n_new, wave_tok + TW) - 1);
-    const int wave_lo = wave_min - w.window + 1, wave_hi = wave_max - w.window + 1;   // the first position of the first token's window, the last's
+    const int wave_hi = wave_max - w.window + 1;      // the first position of the window of the wave's last token
+    // units that all of its columns see (of the windows), and those that some see: of the sinks, and those
+    const int full0 = __builtin_amdgcn_readfirstlane(see.first + (max(wave_hi - see.start, 0) + 15) / 16);
+    const int full1 = __builtin_amdgcn_readfirstlane(none ? 0 : see.first + max(wave_min + 1 - see.start, 0) / 16);
+    const int some0 = __builtin_amdgcn_readfirstlane(see.first + max(wave_min - w.window + 1 - see.start, 0) / 16);
+    const int some1 = __builtin_amdgcn_readfirstlane(none ? 0 : see.unit_of(wave_max) + 1);
+    const int sunk = see.start > 0 ? see.first : (min(w.sinks, see.end) + 15) / 16;   // (where the first token's window reaches the sinks, positions are units)
 
     const table_ptr table = (table_ptr)(uintptr_t)(a.block_table + (size_t)r * a.max_blocks);
     const uint32_t tile_bytes = (uint32_t)a.block_size * D * 2;
@@ -89,12 +113,20 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void window_
     const size_t head_off = ((size_t)a.layer * a.num_kv_heads + g) * tile_bytes;
     const char *kp = static_cast<const char *>(a.k_pool) + head_off, *vp = static_cast<const char *>(a.v_pool) + head_off;
     const uint32_t last_block = (uint32_t)a.num_blocks - 1;
-    const auto unit_at = [&](int u) { return see.at(min(u, last_unit)); };
-    uint32_t ent[2 * GRP];
-    // (an entry that names no block of the pool reads the last one: the rows are meaningless)
-    const auto lookup = [&](int grp, uint32_t (&e)[2 * GRP]) {
+    // A group's units: the blocks they lie in, looked up an iteration before the loads that use them, and where in a block's tile.
+    struct Places {
+        uint32_t block[2 * GRP], at[2 * GRP];
+    };
+    const auto lookup = [&](int grp) {
+        Places x;
 #pragma unroll
-        for (int i = 0; i < 2 * GRP; ++i) e[i] = min((uint32_t)table[unit_at(grp * 2 * GRP + i) >> a.log2_block_size], last_block);
+        for (int i = 0; i < 2 * GRP; ++i) {
+            const int t = see.at(min(grp * 2 * GRP + i, last_unit));
+            // (an entry that names no block of the pool reads the last one: the rows are meaningless)
+            x.block[i] = min((uint32_t)table[t >> a.log2_block_size], last_block);
+            x.at[i] = (uint32_t)((t & (a.block_size - 1)) >> 4) * SUBB;
+        }
+        return x;
     };
     // This lane's part of a load: unit x of a sub-tile to LDS slot x (tiled layout), or slot s of row r takes unit s ^ r of a key row and s ^ 2 r of a
     // value row (plain), so that the rows that an operand read touches lie in different banks.
@@ -105,30 +137,31 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void window_
         lane_k[k] = (uint32_t)(TILED ? x : row * NU + (sl ^ (row & (NU - 1)))) * 16;
         lane_v[k] = (uint32_t)(TILED ? x : row * NU + (sl ^ ((2 * row) & (NU - 1)))) * 16;
     }
-    const auto dma = [&](int st, char *buf, uint32_t e0, uint32_t e1) {
+    const auto dma_group = [&](char *buf, const Places &x) {
 #pragma unroll
-        for (int k = 0; k < LPT; ++k) {
-            const int x0 = kThreads * k + 64 * wv, sub = U >= kThreads ? (kThreads * k) / U : __builtin_amdgcn_readfirstlane(x0 / U);
-            const int t = __builtin_amdgcn_readfirstlane(unit_at(2 * st + sub));
-            const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(sub ? e1 : e0)) * block_stride + (uint32_t)(((t & (a.block_size - 1)) >> 4) * SUBB);
-            typedef __attribute__((address_space(3))) char *lptr;
-            const uint32_t lk = (uint32_t)(uintptr_t)(lptr)(buf + x0 * 16), lv = lk + VOFF;
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lk), "v"(lane_k[k]), "s"(kp + off) : "memory");
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lv), "v"(lane_v[k]), "s"(vp + off) : "memory");
-        }
-    };
-    const auto dma_group = [&](int grp, char *buf, const uint32_t (&e)[2 * GRP]) {
+        for (int h = 0; h < GRP; ++h)
 #pragma unroll
-        for (int h = 0; h < GRP; ++h) dma(grp * GRP + h, buf + h * STAGE, e[2 * h], e[2 * h + 1]);
+            for (int k = 0; k < LPT; ++k) {
+                const int x0 = kThreads * k + 64 * wv;   // the wave's first unit: sub-tile x0 / U
+                const bool second = U >= kThreads ? (kThreads * k) / U != 0 : __builtin_amdgcn_readfirstlane(x0 / U) != 0;
+                const uint32_t block = __builtin_amdgcn_readfirstlane((int)(second ? x.block[2 * h + 1] : x.block[2 * h]));
+                const uint64_t off = (uint64_t)block * block_stride + (second ? x.at[2 * h + 1] : x.at[2 * h]);
+                typedef __attribute__((address_space(3))) char *lptr;
+                const uint32_t lk = (uint32_t)(uintptr_t)(lptr)(buf + h * STAGE + x0 * 16), lv = lk + VOFF;
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lk), "v"(lane_k[k]), "s"(kp + off) : "memory");
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lv), "v"(lane_v[k]), "s"(vp + off) : "memory");
+            }
     };
     const int grp0 = st0 / GRP, grp1 = st0 < st1 ? (st1 + GRP - 1) / GRP : grp0;   // (a part that is not empty begins with a group)
-    {
-        uint32_t e0[2 * GRP], e1[2 * GRP];
-        lookup(grp0, e0);
-        lookup(grp0 + 1, e1);
-        dma_group(grp0, lds, e0);
-        dma_group(grp0 + 1, lds + GSTAGE, e1);
-    }
+    const auto ask_first = [&]() {
+        Places x[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) x[i] = lookup(grp0 + i);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) dma_group(lds + i * GSTAGE, x[i]);
+    };
+    // The first tiles in front of the queries, or, where four groups are on their way, behind them.
+    if constexpr (NB == 2) ask_first();
 
     // this lane's column in each block: (token, head), its position, its queries (of a negative scale: their negatives)
     int pos[kCB];
@@ -150,6 +183,7 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void window_
             qb[b][i] = __builtin_bit_cast(bf16x8, t);
         }
     }
+    if constexpr (NB > 2) ask_first();
     float m[kCB];
     f32x4 o[kCB][NS], l[kCB];
 #pragma unroll
@@ -211,17 +245,43 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void window_
         const int lim = p - t - 4 * qd;
         return (e <= lim) & ((e > lim - w.window) | (e < w.sinks - t - 4 * qd));
     };
-    const auto softmax = [&](int t0, int t1, bool masked) {
+    // The mask of a unit: by what it takes for the wave's columns, most often one of the two comparisons or none.
+    const auto mask = [&](f32x4 (&x)[kCB], int t) {
+        const bool late = t + 15 > wave_min, early = t < wave_hi, sunk = t < w.sinks;
+        if (early & sunk) {
+#pragma unroll
+            for (int b = 0; b < kCB; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (!visible(pos[b], t, e)) x[b][e] = -INFINITY;
+            return;
+        }
+        if (late) {
+#pragma unroll
+            for (int b = 0; b < kCB; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e > pos[b] - t - 4 * qd) x[b][e] = -INFINITY;
+        }
+        if (early) {
+#pragma unroll
+            for (int b = 0; b < kCB; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e <= pos[b] - t - 4 * qd - w.window) x[b][e] = -INFINITY;
+        }
+    };
+    const auto position = [&](int u) { return u <= last_unit ? see.at(u) : 0x40000000; };   // (past the last unit: where nobody looks)
+    const auto softmax = [&](int u, bool masked) {
+        if (masked) {
+            mask(sc0, position(u));
+            mask(sc1, position(u + 1));
+        }
 #pragma unroll
         for (int b = 0; b < kCB; ++b) {
             float sc[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) sc[e] = e < 4 ? sc0[b][e] : sc1[b][e - 4];
-            if (masked) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (!visible(pos[b], e < 4 ? t0 : t1, e & 3)) sc[e] = -INFINITY;
-            }
             float mx = sc[0];                         // (the median with infinity: the maximum)
 #pragma unroll
             for (int e = 1; e < 8; ++e) mx = __builtin_amdgcn_fmed3f(mx, sc[e], INFINITY);
@@ -244,18 +304,14 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void window_
             for (int e = 0; e < 8; ++e) pw[b][e] = (__bf16)fast_exp2(fmaf(sc[e], scale, -mn));
         }
     };
-    // Whether one of the stage's values is no finite number: exponents of all ones, two to a word.
+    // Whether one of the stage's values is no finite number: those give NaN times zero, which the matrix cores find for a few cycles
+    // (by exponents, two operations on each of the registers, a masked stage took 1.3 times as long).
     const auto wild = [&]() {
-        typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
-        u16x2 most = {0, 0};
+        f32x4 y = {0.f, 0.f, 0.f, 0.f};
+        const bf16x8 zero = __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0));
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            const uint4 u = __builtin_bit_cast(uint4, vop[s]);
-            const uint32_t x[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, x[k] & 0x7FFF7FFFu));
-        }
-        return __any((most[0] >= 0x7F80) | (most[1] >= 0x7F80)) != 0;
+        for (int s = 0; s < NS; ++s) y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop[s], zero, y, 0, 0, 0);
+        return __any((y[0] + y[1]) + (y[2] + y[3]) != 0.0f) != 0;
     };
     const auto sums = [&]() {
 #pragma unroll
@@ -269,7 +325,8 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void window_
             for (int b = 0; b < kCB; ++b) o[b][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop[s], pw[b], o[b][s], 0, 0, 0);
     };
     // Token by token: what one does not see is zeroed, and its columns take the result.
-    const auto accumulate_apart = [&](int t0, int t1) {
+    const auto accumulate_apart = [&](int u) {
+        const int t0 = position(u), t1 = position(u + 1);
         sums();
 #pragma unroll 1
         for (int tok = 0; tok < TW; ++tok) {
@@ -280,11 +337,11 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void window_
                 keep[k] = (visible(p, k < 2 ? t0 : t1, 2 * (k & 1)) ? 0x0000FFFFu : 0u) | (visible(p, k < 2 ? t0 : t1, 2 * (k & 1) + 1) ? 0xFFFF0000u : 0u);
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
-                uint4 u = __builtin_bit_cast(uint4, vop[s]);
-                u.x &= keep[0]; u.y &= keep[1]; u.z &= keep[2]; u.w &= keep[3];
+                uint4 v = __builtin_bit_cast(uint4, vop[s]);
+                v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
 #pragma unroll
                 for (int b = 0; b < kCB; ++b) {
-                    const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u), pw[b], o[b][s], 0, 0, 0);
+                    const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), pw[b], o[b][s], 0, 0, 0);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[b][s][e] = pos[b] == p ? y[e] : o[b][s][e];
                 }
@@ -292,38 +349,38 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void window_
         }
     };
 
-    lookup(grp0 + NB, ent);
-    __builtin_amdgcn_s_waitcnt(vmcnt(0));
-    __syncthreads();
+    Places next = lookup(grp0 + NB);
+    // Group `ahead` behind it on its way, this one is there, for everyone.
+    const auto landed = [&](auto ahead) {
+        __builtin_amdgcn_s_waitcnt(vmcnt(ahead * kLoads));
+        __syncthreads();
+    };
+    landed(std::integral_constant<int, NB == 2 ? 0 : NB - 1>{});
     if (!kLean) read_k(lds);
     for (int grp = grp0; grp < grp1; ++grp) {
-        char *cur = lds + ((grp - grp0) & 1) * GSTAGE, *nxt = lds + ((grp - grp0 + 1) & 1) * GSTAGE;
+        char *cur = lds + ((grp - grp0) & (NB - 1)) * GSTAGE, *nxt = lds + ((grp - grp0 + 1) & (NB - 1)) * GSTAGE;
 #pragma unroll
         for (int h = 0; h < GRP; ++h) {
             const int st = grp * GRP + h;
             char *buf = cur + h * STAGE;
-            // the stage's units; one past the last: positions that nobody sees
-            const int t0 = unit_at(2 * st), t1 = 2 * st + 1 <= last_unit ? see.at(2 * st + 1) : 0x40000000;
-            const auto some = [&](int t) { return (t <= wave_max) & ((t + 15 >= wave_lo) | (t < w.sinks)); };
-            const auto every = [&](int t) { return (t + 15 <= wave_min) & ((t >= wave_hi) | (t + 16 <= w.sinks)); };
-            const bool live = (st < st1) & (some(t0) | some(t1));   // wave-uniform: its columns see something of it
-            const bool masked = !(every(t0) & every(t1));
+            const int u = 2 * st;                     // its first unit; what follows is uniform over the wave
+            const bool live = (st < st1) & (u < some1) & ((u + 1 >= some0) | (u < sunk));
+            const bool masked = (u < full0) | (u + 2 > full1);
             bool apart = false;
             if (live) {
                 if (kLean) read_k(buf);
                 else read_v(buf);                     // needed after the next K operands are asked for
                 scores();
                 if (kLean) read_v(buf);
-                softmax(t0, t1, masked);
+                softmax(u, masked);
                 // (here, where no keys are held in registers)
                 apart = masked && wild();
-                if (apart) accumulate_apart(t0, t1);
+                if (apart) accumulate_apart(u);
             }
             if (h == GRP - 1) {
-                __builtin_amdgcn_s_waitcnt(vmcnt(0)); // the next group is there, for everyone; this one's operands are in registers
-                __syncthreads();
-                dma_group(grp + NB, cur, ent);
-                lookup(grp + NB + 1, ent);
+                landed(std::integral_constant<int, NB - 2>{});   // this group's operands are in registers: its place is free
+                dma_group(cur, next);
+                next = lookup(grp + NB + 1);
             }
             if (!kLean && st + 1 < grp1 * GRP) read_k(h == GRP - 1 ? nxt : buf + STAGE);
             if (live && !apart) accumulate();
@@ -348,50 +405,100 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void window_
     }
 }
 
-// Adds the parts of a tile up: a workgroup takes 16 columns of one, its waves a quarter of the dims each (a slab at least).
-template <int D, int kCB>
+// Adds the parts of a tile up, two slabs of 16 columns at a time: a wave alone where there are up to four parts, else the four waves of a workgroup every
+// fourth part each (16 parts of 8 tiles 7.0 us alone, 4.0 together; 2 parts of 300 tiles 7.8 and 13).  What they add is asked for in front of the
+// lengths that say which rows it is (where it lies goes by the launch alone).
+template <int D, int kCB, bool ALONE>
 __global__ __launch_bounds__(kThreads) void window_join(const WindowArgs w0)
 {
-    constexpr int kCols = 16 * kCB, NS = D / 16, EACH = NS / kWaves < 2 ? 2 : NS / kWaves, N = 4;
+    constexpr int kCols = 16 * kCB, N = 4, MOST = kMostParts / kWaves;
+    __shared__ float4 sums[kWaves][2][64];
+    __shared__ float2 stats[kWaves][64];
     const DecodeArgs &a = w0.d;
     WindowArgs w = w0;
     w.parts = 1;
     const int G = a.num_q_heads / a.num_kv_heads, TW = kCols / G, WT = kWaves * TW, parts = w0.parts;
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 15, qd = lane >> 4;
-    TileAt at;
-    if (wv * EACH >= NS || !tile_at<kThreads>(w, WT, at)) return;
-    const int n_new = min(at.n_new, w.total_tokens - at.first), block = blockIdx.y;
-    const int wave = block / kCB, c = block % kCB * 16 + j, tl = c / G, tok = at.tile * WT + wave * TW + tl;
-    if (at.tile * WT + wave * TW >= n_new) return;    // (a wave that had no tokens has left nothing)
-    const bool mine = c < TW * G && tok < n_new;
+    constexpr int STEP = ALONE ? 1 : kWaves;
+    const int block = blockIdx.y, slab = 2 * (ALONE ? blockIdx.z * kWaves + wv : blockIdx.z), from0 = ALONE ? 0 : wv;
+    if (slab >= D / 16) return;
     const size_t state = tile_state_floats(D, kWaves * kCols);
-    const float *x = a.partials + (size_t)at.item * parts * state;
+    const int item = tile_item(w, blockIdx.x);
+    if (item < 0) return;
+    const float *x = a.partials + (size_t)item * parts * state;
     float M = kLeast, L = 0.0f;
-    f32x4 A[EACH];
+    f32x4 A[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    const auto add = [&](float2 ml, f32x4 y0, f32x4 y1) {
+        const float Mn = fmaxf(M, ml.x), f0 = fast_exp2(M - Mn), f = fast_exp2(ml.x - Mn);
+        L = L * f0 + ml.y * f;
 #pragma unroll
-    for (int s = 0; s < EACH; ++s) A[s] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int k0 = 0; k0 < parts; k0 += N) {
+        for (int e = 0; e < 4; ++e) {
+            A[0][e] = A[0][e] * f0 + y0[e] * f;
+            A[1][e] = A[1][e] * f0 + y1[e] * f;
+        }
+        M = Mn;
+    };
+    TileAt at;
+    bool on = false;
+    for (int k0 = 0; k0 < MOST; k0 += N) {
         float2 ml[N];
-        f32x4 y[N][EACH];
+        f32x4 y[N][2];
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const float *from = x + (size_t)min(k0 + k, parts - 1) * state;
+            const float *from = x + (size_t)min(from0 + STEP * (k0 + k), parts - 1) * state;
             ml[k] = *reinterpret_cast<const float2 *>(from + (size_t)kWaves * kCols * D + 2 * (block * 16 + j));
 #pragma unroll
-            for (int s = 0; s < EACH; ++s) y[k][s] = *reinterpret_cast<const f32x4 *>(from + (size_t)block * 16 * D + (wv * EACH + s) * 256 + 4 * lane);
+            for (int s = 0; s < 2; ++s) y[k][s] = *reinterpret_cast<const f32x4 *>(from + (size_t)block * 16 * D + (slab + s) * 256 + 4 * lane);
+        }
+        if (k0 == 0) {
+            on = tile_at(w, WT, at);
+            if (!on) return;
         }
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            if (k0 + k >= parts) break;
-            const float Mn = fmaxf(M, ml[k].x), f0 = fast_exp2(M - Mn), f = fast_exp2(ml[k].x - Mn);
-            L = L * f0 + ml[k].y * f;
+        for (int k = 0; k < N; ++k)
+            if (from0 + STEP * (k0 + k) < parts) add(ml[k], y[k][0], y[k][1]);
+        if (STEP * (k0 + N) >= parts) break;
+    }
+    if constexpr (!ALONE) {
+        sums[wv][0][lane] = make_float4(A[0][0], A[0][1], A[0][2], A[0][3]);
+        sums[wv][1][lane] = make_float4(A[1][0], A[1][1], A[1][2], A[1][3]);
+        stats[wv][lane] = make_float2(M, L);
+        __syncthreads();
+        if (wv > 0) return;
 #pragma unroll
-            for (int s = 0; s < EACH; ++s)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) A[s][e] = A[s][e] * f0 + y[k][s][e] * f;
-            M = Mn;
+        for (int k = 1; k < kWaves; ++k) {
+            const float4 y0 = sums[k][0][lane], y1 = sums[k][1][lane];
+            add(stats[k][lane], f32x4{y0.x, y0.y, y0.z, y0.w}, f32x4{y1.x, y1.y, y1.z, y1.w});
         }
     }
-    uint16_t *to = static_cast<uint16_t *>(a.out) + ((size_t)(at.first + (mine ? tok : 0)) * a.num_q_heads + at.g * G + (mine ? c - tl * G : 0)) * D + 16 * wv * EACH;
-    store_column<EACH>(to, qd, mine, 1.0f / L, A);
+    const int n_new = min(at.n_new, w.total_tokens - at.first);
+    const int wave_tok = at.tile * WT + block / kCB * TW, c = block % kCB * 16 + j, tl = c / G;
+    // (a wave that had no tokens has left nothing)
+    const bool mine = c < TW * G && wave_tok + tl < n_new;
+    uint16_t *to = static_cast<uint16_t *>(a.out) + ((size_t)(at.first + (mine ? wave_tok + tl : 0)) * a.num_q_heads + at.g * G + (mine ? c - tl * G : 0)) * D + 16 * slab;
+    store_column<2>(to, qd, mine, 1.0f / L, A);
+}
+
+// ---------------------------------------------------------------- two teams of waves
+
+// prefill_teams' way through a tile of 256 columns, for launches with many new tokens.
+template <int D, bool TILED, int kCB>
+__global__ __launch_bounds__(512, 2) void window_teams(const WindowArgs w)
+{
+    constexpr bool WINDOW = true;
+    constexpr int W = 8, kCols = 16 * kCB;
+    constexpr int NK = D / 32, NS = D / 16, U = D * 2, NU = D / 8;
+    constexpr int SUBB = 16 * D * 2, VOFF = 2 * SUBB, STAGE = 4 * SUBB;
+    constexpr int NB = 131072 / STAGE;
+    constexpr int VA = NB - 2, KA = NB == 4 ? NB : NB - 2;
+    constexpr int NE = U / 256;
+    static_assert(D == 128, "a stage's values are all in registers before they are multiplied");
+    extern __shared__ __align__(16) char lds[];
+
+    const DecodeArgs &a = w.d;
+    const int G = a.num_q_heads / a.num_kv_heads, TW = kCols / G, WT = W * TW, window = w.window, sinks = w.sinks;
+    TileAt at;
+    if (!tile_at(w, WT, at)) return;
+    const int r = at.r, g = at.g, tile = at.tile, first = at.first, n_new = min(at.n_new, w.total_tokens - first), C = at.ctx - at.n_new + n_new;
+#include "teams_body.h"
 }

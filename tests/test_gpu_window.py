@@ -24,6 +24,8 @@ CASES = [
     ("bf16", 8, 2, 128, 16, [(700, 700), (1200, 37)], [(260, 4), (97, 70)]),       # several tiles of new tokens
     ("bf16", 4, 4, 128, 16, [(700, 700), (1200, 37)], [(260, 4)]),
     ("bf16", 8, 4, 64, 16, [(900, 30), (700, 1), (1500, 100)], [(512, 16)]),
+    ("bf16", 16, 8, 128, 16, [(3000, 2500), (2800, 2800), (500, 1), (40, 0), (1700, 1600)], [(150, 20), (1000, 3)]),   # two teams of waves
+    ("bf16", 10, 10, 128, 32, [(3000, 2500), (2900, 2900), (700, 700), (1700, 1600)], [(33, 0), (700, 40)]),
     ("f32", 4, 4, 64, 16, [(40, 40), (117, 3), (64, 1), (9, 0), (33, 33)], [(1, 0), (13, 3), (30, 20), (200, 5)]),
     ("f32", 8, 2, 32, 16, [(150, 150), (80, 7)], [(11, 2), (64, 16)]),
     ("f32", 8, 2, 128, 32, [(130, 130), (300, 9)], [(50, 4)]),
