@@ -15,18 +15,6 @@
 #include "requests.h"
 #include "tile_parts.h"
 
-#ifndef WTEAM
-#define WTEAM 256
-#endif
-#ifndef WPT
-#define WPT 512
-#endif
-#ifndef WPS
-#define WPS 4
-#endif
-#ifndef WCB
-#define WCB 512
-#endif
 namespace lamps {
 namespace {
 
@@ -423,6 +411,7 @@ __global__ __launch_bounds__(kThreads) void window_rows(const WindowArgs w)
 }
 
 #include "window_tiles.h"
+#include "window_tiles_f32.h"
 
 // ---------------------------------------------------------------- launches
 
@@ -474,10 +463,11 @@ hipError_t launch_tiles(WindowArgs w, hipStream_t s)
     const long long items = (long long)w.total_tokens / WT + a.batch, tiles = items * a.num_kv_heads;
     const long long stages = (std::min((long long)a.max_blocks * a.block_size, (long long)w.window + w.sinks + WT) + 31) / 32 + 1;
     const long long state = (long long)tile_state_floats(D, kWaves * 16 * kCB) * (long long)sizeof(float);
-    // two workgroups fit a CU; four stages at least to a part
+    // Two workgroups fit a CU, 512 the chip: with twice as many parts 12 responses of 4 to 64 tokens, window 2 048, took 49 us, 45 so, and one prompt of 2 000 (504
+    // tiles) 53 us, 31 whole.  Four stages at least to a part: a part's way to its first product is as long as four.
     // (about as many tiles as there are: half of the requests' last ones are there besides the full ones)
     const long long there = std::max(1LL, ((long long)w.total_tokens / WT + a.batch / 2) * a.num_kv_heads);
-    long long parts = std::min(WPT / there, stages / WPS);
+    long long parts = std::min(512 / there, stages / 4);
     parts = std::max(1LL, std::min({parts, (long long)kMostParts, (long long)a.partial_capacity / (state * tiles)}));
     const long long grid = (tiles * parts + 7) / 8 * 8, join = (tiles + 7) / 8 * 8;
     if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
@@ -497,7 +487,7 @@ hipError_t launch_tiles(WindowArgs w, hipStream_t s)
     return hipGetLastError();
 }
 
-template <int D, bool TILED, int kCB>
+template <int D, int kCB>
 hipError_t launch_teams(WindowArgs w, hipStream_t s)
 {
     const int WT = 8 * (16 * kCB / (w.d.num_q_heads / w.d.num_kv_heads));
@@ -505,7 +495,7 @@ hipError_t launch_teams(WindowArgs w, hipStream_t s)
     if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
     w.items = (int)items;
     w.parts = 1;
-    hipLaunchKernelGGL((window_teams<D, TILED, kCB>), dim3((unsigned)grid), dim3(512), 128 << 10, s, w);
+    hipLaunchKernelGGL((window_teams<D, kCB>), dim3((unsigned)grid), dim3(512), 128 << 10, s, w);
     return hipGetLastError();
 }
 
@@ -513,15 +503,36 @@ template <int D, bool TILED>
 hipError_t launch_tiles(const WindowArgs &w, hipStream_t s)
 {
     const int G = w.d.num_q_heads / w.d.num_kv_heads;
-    if constexpr (D == 128) {
+    const long long walk = std::min((long long)w.window, (long long)w.d.max_blocks * w.d.block_size);
+    if constexpr (D == 128 && TILED) {
+        // Two teams: with grouped heads, where a walk is eight times a tile's own tokens and more, requests fill four tiles and there is one to a CU (time over that of tiles
+        // of 128 columns, 32 / 8 heads, window 1 024 / 256: one prompt of 4 096 0.89 / 1.08, 16 of 512 0.95 / 1.01, 8 of 256 on 3 000 0.86 / 1.0,
+        // 16 of 128 on 3 000 1.13 / 1.34; 40 plain heads, prompts, windows of 64 to 4 096: 1.03 to 1.3).
         const int WT = 256 / G;
-        if (w.d.scale_log2e > 0.0f && w.d.num_kv_heads * ((long long)w.total_tokens / WT) >= WTEAM) return launch_teams<D, TILED, 2>(w, s);
+        if (G <= 32 && w.d.scale_log2e > 0.0f && walk >= 8 * WT && w.total_tokens >= 4LL * WT * w.d.batch && w.d.num_kv_heads * ((long long)w.total_tokens / WT) >= 256)
+            return launch_teams<D, 2>(w, s);
     }
     if constexpr (D >= 256) {                         // (as in prefill_mfma)
         return launch_tiles<D, TILED, TILED ? 2 : 1>(w, s);
     } else {
-        return G > 16 || (long long)w.max_new_tokens * G > WCB ? launch_tiles<D, TILED, 2>(w, s) : launch_tiles<D, TILED, 1>(w, s);
+        // Tiles of 64 columns, of which more fit a CU: where requests have few columns, and where a tile's own tokens are a large part of what it walks over (time over that
+        // of 128, prompts: window 64, 40 plain heads 0.88, 32 / 8 heads 0.91 to 0.96; 256, 0.93 and 1.03 to 1.07; 1 024, 1.04 and 1.07 to 1.13;
+        // 8 of 256 on 3 000, 32 / 8 heads, 1.2 to 1.3).
+        const bool narrow = G <= 16 && ((long long)w.max_new_tokens * G <= 512 || walk * G <= 512);
+        return narrow ? launch_tiles<D, TILED, 1>(w, s) : launch_tiles<D, TILED, 2>(w, s);
     }
+}
+
+template <int D>
+hipError_t launch_tiles_f32(WindowArgs w, hipStream_t s)
+{
+    const int GH = f32_heads(w.d.num_q_heads / w.d.num_kv_heads), TW = 16 / GH;
+    const long long items = (long long)w.total_tokens / TW + w.d.batch, grid = (items * (w.d.num_q_heads / GH) + 7) / 8 * 8;
+    if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
+    w.items = (int)items;
+    w.parts = 1;
+    hipLaunchKernelGGL(window_tiles_f32<D>, dim3((unsigned)grid), dim3(kThreads), 0, s, w);
+    return hipGetLastError();
 }
 
 template <int LPT>
@@ -575,6 +586,11 @@ hipError_t launch_prefill_window(const WindowArgs &w, hipStream_t stream)
         if (a.head_dim == 64) return tiled ? launch_tiles<64, true>(w, stream) : launch_tiles<64, false>(w, stream);
         if (a.head_dim == 128) return tiled ? launch_tiles<128, true>(w, stream) : launch_tiles<128, false>(w, stream);
         if (a.head_dim == 256) return tiled ? launch_tiles<256, true>(w, stream) : launch_tiles<256, false>(w, stream);
+    }
+    if (!a.bf16 && !w.force_rows) {
+        if (a.head_dim == 32) return launch_tiles_f32<32>(w, stream);
+        if (a.head_dim == 64) return launch_tiles_f32<64>(w, stream);
+        if (a.head_dim == 128) return launch_tiles_f32<128>(w, stream);
     }
     return launch_window(w, stream);
 }

@@ -14,19 +14,19 @@
 // Which workgroup does what: items -- tiles of one head, numbered by the row that they begin at, at most one for nothing per request -- head by
 // head, and of these an eighth, one after the other, to each of the eight XCDs: neighbours in time and place share most of their windows in an L2.
 struct TileAt {
-    int r, g, tile, first, n_new, ctx, part, item;
+    int r, g, tile, first, n_new, ctx, part, item;    // (g: of `heads` that tiles are dealt for)
 };
 // The number of a workgroup's item, part by part; < 0: none.
-__device__ __forceinline__ int tile_item(const WindowArgs &w, unsigned block)
+__device__ __forceinline__ int tile_item(const WindowArgs &w, unsigned block, int heads)
 {
-    const unsigned all = (unsigned)w.items * (unsigned)w.d.num_kv_heads * (unsigned)w.parts, per = (all + 7) / 8, i = (block & 7) * per + (block >> 3);
+    const unsigned all = (unsigned)w.items * (unsigned)heads * (unsigned)w.parts, per = (all + 7) / 8, i = (block & 7) * per + (block >> 3);
     return block >> 3 < per && i < all ? (int)i : -1;
 }
-__device__ __forceinline__ bool tile_at(const WindowArgs &w, int WT, TileAt &at)
+__device__ __forceinline__ bool tile_at(const WindowArgs &w, int WT, TileAt &at, int heads)
 {
     const DecodeArgs &a = w.d;
     const unsigned items = (unsigned)w.items;
-    const int i0 = tile_item(w, blockIdx.x);
+    const int i0 = tile_item(w, blockIdx.x, heads);
     if (i0 < 0) return false;
     const unsigned i = (unsigned)i0;
     // (uniform, and said to be: divisions go through the vector ALUs, and addresses of loads into LDS are scalars)
@@ -48,25 +48,20 @@ __device__ __forceinline__ bool tile_at(const WindowArgs &w, int WT, TileAt &at)
 
 constexpr size_t tile_state_floats(int D, int columns) { return (size_t)columns * (D + 2); }
 
-// Narrow tiles, of 64 columns: one stage per barrier, operands read one after the other, for three or four workgroups to a CU.
-#ifndef SMALLN
-#define SMALLN 1
-#endif
-#ifndef SMALLS
-#define SMALLS 0
-#endif
+// Narrow tiles, of 64 columns, whole: one stage per barrier, operands read one after the other, for three or four workgroups to a CU.  Shared ones
+// keep four stages in LDS instead (12 responses 43.6 us, 45.2 as whole ones have it).
 template <int D, int kCB, bool SPLIT>
-constexpr bool tile_small() { return D <= 128 && kCB == 1 && (SPLIT ? SMALLS : SMALLN); }
+constexpr bool tile_small() { return D <= 128 && kCB == 1 && !SPLIT; }
 // Stages per barrier, and groups of them that LDS holds.
-template <int D, int kCB, bool SPLIT>
+template <int D, int kCB>
 constexpr int tile_groups() { return D <= 128 && kCB > 1 ? 2 : 1; }
 template <int D, int kCB, bool SPLIT>
-constexpr int tile_buffers() { return D <= 128 && SPLIT && kCB == 1 && !tile_small<D, kCB, SPLIT>() ? 4 : 2; }
+constexpr int tile_buffers() { return D <= 128 && SPLIT && kCB == 1 ? 4 : 2; }
 
 template <int D, bool TILED, int kCB, bool SPLIT>
 __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : (tile_small<D, kCB, SPLIT>()) ? (D == 128 && TILED ? 3 : 4) : 2) void window_tiles(const WindowArgs w)
 {
-    constexpr int kCols = 16 * kCB, GRP = tile_groups<D, kCB, SPLIT>(), NB = tile_buffers<D, kCB, SPLIT>();
+    constexpr int kCols = 16 * kCB, GRP = tile_groups<D, kCB>(), NB = tile_buffers<D, kCB, SPLIT>();
     constexpr int NK = D / 32, NS = D / 16, U = D * 2, NU = D / 8;
     constexpr int LPT = (2 * U) / kThreads;           // 16-byte units per thread, pool and stage
     constexpr int SUBB = 16 * D * 2, VOFF = 2 * SUBB, STAGE = 4 * SUBB, GSTAGE = GRP * STAGE;
@@ -78,7 +73,7 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : (tile_small<D, 
     const DecodeArgs &a = w.d;
     const int G = a.num_q_heads / a.num_kv_heads, TW = kCols / G, WT = kWaves * TW;
     TileAt at;
-    if (!tile_at(w, WT, at)) return;
+    if (!tile_at(w, WT, at, a.num_kv_heads)) return;
     const int r = at.r, g = at.g, first = at.first, base_pos = at.ctx - at.n_new;
     const int n_new = min(at.n_new, w.total_tokens - first);
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -423,7 +418,7 @@ __global__ __launch_bounds__(kThreads) void window_join(const WindowArgs w0)
     const int block = blockIdx.y, slab = 2 * (ALONE ? blockIdx.z * kWaves + wv : blockIdx.z), from0 = ALONE ? 0 : wv;
     if (slab >= D / 16) return;
     const size_t state = tile_state_floats(D, kWaves * kCols);
-    const int item = tile_item(w, blockIdx.x);
+    const int item = tile_item(w, blockIdx.x, a.num_kv_heads);
     if (item < 0) return;
     const float *x = a.partials + (size_t)item * parts * state;
     float M = kLeast, L = 0.0f;
@@ -451,7 +446,7 @@ __global__ __launch_bounds__(kThreads) void window_join(const WindowArgs w0)
             for (int s = 0; s < 2; ++s) y[k][s] = *reinterpret_cast<const f32x4 *>(from + (size_t)block * 16 * D + (slab + s) * 256 + 4 * lane);
         }
         if (k0 == 0) {
-            on = tile_at(w, WT, at);
+            on = tile_at(w, WT, at, a.num_kv_heads);
             if (!on) return;
         }
 #pragma unroll
@@ -481,11 +476,11 @@ __global__ __launch_bounds__(kThreads) void window_join(const WindowArgs w0)
 
 // ---------------------------------------------------------------- two teams of waves
 
-// prefill_teams' way through a tile of 256 columns, for launches with many new tokens.
-template <int D, bool TILED, int kCB>
+// prefill_teams' way through a tile of 256 columns, for launches with many new tokens (grouped heads: plain ones are as fast or faster by window_tiles).
+template <int D, int kCB>
 __global__ __launch_bounds__(512, 2) void window_teams(const WindowArgs w)
 {
-    constexpr bool WINDOW = true;
+    constexpr bool WINDOW = true, TILED = true;
     constexpr int W = 8, kCols = 16 * kCB;
     constexpr int NK = D / 32, NS = D / 16, U = D * 2, NU = D / 8;
     constexpr int SUBB = 16 * D * 2, VOFF = 2 * SUBB, STAGE = 4 * SUBB;
@@ -498,7 +493,7 @@ __global__ __launch_bounds__(512, 2) void window_teams(const WindowArgs w)
     const DecodeArgs &a = w.d;
     const int G = a.num_q_heads / a.num_kv_heads, TW = kCols / G, WT = W * TW, window = w.window, sinks = w.sinks;
     TileAt at;
-    if (!tile_at(w, WT, at)) return;
+    if (!tile_at(w, WT, at, a.num_kv_heads)) return;
     const int r = at.r, g = at.g, tile = at.tile, first = at.first, n_new = min(at.n_new, w.total_tokens - first), C = at.ctx - at.n_new + n_new;
 #include "teams_body.h"
 }
