@@ -50,6 +50,7 @@ class LampsRope(ctypes.Structure):
         super().__init__(rotary_dim, pairs, 1 if normalise else 0, norm_eps, amplitude, _ptr(frequencies) or None,
                          _ptr(q_weight) or None, _ptr(k_weight) or None)
         self._keep = (frequencies, q_weight, k_weight)
+        self.address = ctypes.addressof(self)
 
 
 def lib_path():
@@ -99,8 +100,8 @@ def load_library():
         "lamps_decode_attn_window": [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp],
         "lamps_prefill_attn_window": [vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp],
         "lamps_rope_frequencies": [i32, f64, i32, f64, f64, f64, f64, vp],
-        "lamps_rope_append": [vp, i32, i32, ctypes.POINTER(LampsRope), vp, i64, vp, i64, vp, i64, vp, vp, vp, i32, vp],
-        "lamps_rope_append_tokens": [vp, i32, i32, i32, ctypes.POINTER(LampsRope), vp, i64, vp, i64, vp, i64, vp, vp, vp, vp],
+        "lamps_rope_append": [vp, i32, i32, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, i32, vp],
+        "lamps_rope_append_tokens": [vp, i32, i32, i32, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp],
         "lamps_batch_tables": [vp, i32, i32, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp],
         "lamps_swap_out": [vp, vp, i32, vp, ctypes.POINTER(u64)],
         "lamps_swap_in": [vp, vp, vp, i32, ctypes.POINTER(u64)],
@@ -262,12 +263,14 @@ class LampsSched:
 
 
 def _ptr(x):
+    try:                                # (a tensor, most often; in front of the rest: a call has up to eleven of them)
+        return x.data_ptr()
+    except AttributeError:
+        pass
     if x is None:
         return None
     if isinstance(x, int):
         return x
-    if hasattr(x, "data_ptr"):
-        return x.data_ptr()
     if hasattr(x, "ctypes"):            # numpy array
         return x.ctypes.data
     return ctypes.cast(x, ctypes.c_void_p).value
@@ -390,13 +393,13 @@ class Lamps:
     def rope_append(self, layer, batch, rope, q, k_new, v_new, block_table, ctx_lens, running_mask, advance, q_out,
                     q_stride=0, k_stride=0, v_stride=0):
         """Strides in elements; 0: rows follow each other (they are not taken from a tensor's own strides)."""
-        self._check(self.lib.lamps_rope_append(self.h, layer, batch, rope, _ptr(q), q_stride, _ptr(k_new), k_stride, _ptr(v_new),
+        self._check(self.lib.lamps_rope_append(self.h, layer, batch, rope.address, _ptr(q), q_stride, _ptr(k_new), k_stride, _ptr(v_new),
                                                v_stride, _ptr(block_table), _ptr(ctx_lens), _ptr(running_mask),
                                                1 if advance else 0, _ptr(q_out)))
 
     def rope_append_tokens(self, layer, n_req, total_tokens, rope, q, k_new, v_new, q_start, block_table, ctx_lens, q_out,
                            q_stride=0, k_stride=0, v_stride=0):
-        self._check(self.lib.lamps_rope_append_tokens(self.h, layer, n_req, total_tokens, rope, _ptr(q), q_stride, _ptr(k_new),
+        self._check(self.lib.lamps_rope_append_tokens(self.h, layer, n_req, total_tokens, rope.address, _ptr(q), q_stride, _ptr(k_new),
                                                       k_stride, _ptr(v_new), v_stride, _ptr(q_start), _ptr(block_table),
                                                       _ptr(ctx_lens), _ptr(q_out)))
 

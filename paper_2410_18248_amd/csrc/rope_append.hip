@@ -54,6 +54,14 @@ struct Turner {
             s[e] = (a.neighbours ? (e & 1) == 0 : low) ? -x.y : x.y;
         }
     }
+    // What the lane half a head away has: without LDS.
+    static __device__ __forceinline__ float across(float x)
+    {
+        if constexpr (LPH == 32) return __shfl_xor(x, 16);
+        const int y = __builtin_amdgcn_update_dpp(0, __float_as_int(x), LPH == 16 ? 0x128 : 0x141, 0xF, 0xF, true);   // row_ror 8; row_half_mirror
+        if constexpr (LPH == 16) return __int_as_float(y);
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, y, 0x1B, 0xF, 0xF, true));                               // quad_perm [3, 2, 1, 0]
+    }
     // One head's: by the LPH lanes that hold it together.
     __device__ __forceinline__ uint4 apply(const RopeArgs &a, uint4 x, const float (&w)[N]) const
     {
@@ -70,8 +78,16 @@ struct Turner {
         }
         if (a.rotary_dim > 0) {
             float o[N];
+            if (a.neighbours) {                       // uniform
 #pragma unroll
-            for (int e = 0; e < N; ++e) o[e] = a.neighbours ? f[e ^ 1] : __shfl(f[e], other);
+                for (int e = 0; e < N; ++e) o[e] = f[e ^ 1];
+            } else if (a.rotary_dim == LPH * N) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) o[e] = across(f[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) o[e] = __shfl(f[e], other);
+            }
 #pragma unroll
             for (int e = 0; e < N; ++e) f[e] = turned ? fmaf(f[e], c[e], o[e] * s[e]) : f[e];
         }
@@ -203,74 +219,75 @@ __global__ __launch_bounds__((rope_threads<D, BF16>())) void rope_append_tokens(
     const size_t tile = (size_t)bs * D, sub_at = (size_t)(((sub * 16) & (bs - 1)) >> 4) * 16 * D;
     const char *q = static_cast<const char *>(a.q) + (n * a.q_stride + d) * ES, *k = static_cast<const char *>(a.k_new) + (n * a.k_stride + d) * ES;
     char *q_out = static_cast<char *>(a.q_out) + (n * H * D + d) * ES;
-    // queries of heads g0 G .. g1 G - 1, then keys g0 .. g1 - 1
-    const int nq = (g1 - g0) * G, all = nq + g1 - g0;
-    const auto from = [&](int i) { return *reinterpret_cast<const uint4 *>(i < nq ? q + (size_t)(g0 * G + i) * D * ES : k + (size_t)(g0 + i - nq) * D * ES); };
-    for (int i0 = hs; i0 < all; i0 += AHEAD * HS) {
-        uint4 x[AHEAD];
+    // Values.  Plain layout: as keys.  Tiled layout: a wave takes four slots, a quad, of up to 128 dims, 16 bytes of a slot to a lane, and brings them into
+    // the tile's units, four slots of two dims each, by the transposing LDS read (lane j of 16 receives dim j of four rows); a quad that is not all
+    // new goes by 16 bits.
+    constexpr int VROW = D < 128 ? D : 128, VL = VROW / 8;   // dims of a row in a wave's LDS, and the lanes that load one
+    const int lane = tid & 63, wave = tid >> 6;
+    const int vchunk = TILED ? (D < 128 ? 0 : wave % (D / 128)) : 0;                  // which 128 dims
+    const int vfirst = TILED ? (D < 128 ? wave % 2 * 8 : wave / (D / 128) % 4 * 4) : 0;   // the wave's first slot
+    const int vd = TILED ? vchunk * 128 + lane % VL * 8 : d, vslot = TILED ? vfirst + lane / VL : slot;
+    const int vt = sub * 16 + vslot;
+    const bool vlive = vt >= t_lo && vt < t_hi;
+    const char *v = static_cast<const char *>(a.v_new) + (((size_t)first + (vlive ? vt - p0 : t_lo - p0)) * a.v_stride + vd) * ES;
+    __shared__ __align__(16) uint16_t quads[TILED ? THREADS / 64 : 1][TILED ? 512 : 8];
+    const auto put_values = [&](uint4 x, int g) {
+        const size_t at = (((size_t)block * a.num_layers + a.layer) * Hkv + g) * tile + sub_at;
+        if constexpr (!TILED) {
+            if (live) *reinterpret_cast<uint4 *>(static_cast<char *>(a.v_pool) + (at + (size_t)slot * D + d) * ES) = x;
+        } else {
+            typedef __attribute__((address_space(3))) s16x4 *lds_ptr;
+            uint16_t *mine = quads[wave];
+            *reinterpret_cast<uint4 *>(mine + lane * 8) = x;
+            const int i16 = lane & 15, group = lane >> 4;    // the 16 lanes' quad and 32 dims of the wave's
+            const int quad = D < 128 ? group >> 1 : 0, i32 = D < 128 ? group & 1 : group;
+            const uint16_t *from = mine + (quad * 4 + (i16 >> 2)) * VROW + 32 * i32 + 4 * (i16 & 3);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(from + 16));
+            uint16_t *to = static_cast<uint16_t *>(a.v_pool) + at;
+            const int q0 = vfirst + quad * 4, t0 = sub * 16 + q0;
+            if (t0 >= t_lo && t0 + 4 <= t_hi) {
+                const uint2 l = __builtin_bit_cast(uint2, lo), h = __builtin_bit_cast(uint2, hi);
+                *reinterpret_cast<uint4 *>(to + (size_t)(((vchunk * 4 + i32) * 4 + (q0 >> 2)) * 16 + i16) * 8) = make_uint4(l.x, l.y, h.x, h.y);
+            } else {
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) x[u] = from(min(i0 + u * HS, all - 1));
+                for (int e = 0; e < 4; ++e)
+                    if (t0 + e >= t_lo && t0 + e < t_hi) {
+                        uint16_t *unit = to + (size_t)(((vchunk * 4 + i32) * 4 + (q0 >> 2)) * 16 + i16) * 8 + e;
+                        unit[0] = (uint16_t)lo[e];
+                        unit[4] = (uint16_t)hi[e];
+                    }
+            }
+        }
+    };
+    // queries of heads g0 G .. g1 G - 1, keys and values g0 .. g1 - 1: a batch of heads is asked for while the one before it is turned
+    const int nq = (g1 - g0) * G, nk = nq + g1 - g0, all = nk + g1 - g0;
+    const auto from = [&](int i) {
+        return *reinterpret_cast<const uint4 *>(i < nq ? q + (size_t)(g0 * G + i) * D * ES : i < nk ? k + (size_t)(g0 + i - nq) * D * ES : v + (size_t)(g0 + i - nk) * D * ES);
+    };
+    uint4 x[AHEAD], y[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) x[u] = from(min(hs + u * HS, all - 1));
+    for (int i0 = hs; i0 < all; i0 += AHEAD * HS) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) y[u] = from(min(i0 + (AHEAD + u) * HS, all - 1));
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            const int i = i0 + u * HS;
-            if (i >= all) break;                      // (whole waves, or whole heads of one)
+            const int i = i0 + u * HS;                // (the same for a wave)
+            if (i >= all) break;
             if (i < nq) {
-                const uint4 y = turner.apply(a, x[u], qw);
-                if (live) *reinterpret_cast<uint4 *>(q_out + (size_t)(g0 * G + i) * D * ES) = y;
-            } else {
-                const uint4 y = turner.apply(a, x[u], kw);
+                const uint4 z = turner.apply(a, x[u], qw);
+                if (live) *reinterpret_cast<uint4 *>(q_out + (size_t)(g0 * G + i) * D * ES) = z;
+            } else if (i < nk) {
+                const uint4 z = turner.apply(a, x[u], kw);
                 const size_t at = (((size_t)block * a.num_layers + a.layer) * Hkv + g0 + i - nq) * tile + sub_at;
                 const size_t o = TILED ? (size_t)((d >> 3) * 16 + slot) * 8 : (size_t)slot * D + d;
-                if (live) *reinterpret_cast<uint4 *>(static_cast<char *>(a.k_pool) + (at + o) * ES) = y;
-            }
-        }
-    }
-    const char *v = static_cast<const char *>(a.v_new);
-    if constexpr (!TILED) {
-        for (int g = g0 + hs; g < g1; g += HS) {
-            const uint4 x = *reinterpret_cast<const uint4 *>(v + (n * a.v_stride + (size_t)g * D + d) * ES);
-            const size_t at = (((size_t)block * a.num_layers + a.layer) * Hkv + g) * tile + sub_at + (size_t)slot * D + d;
-            if (live) *reinterpret_cast<uint4 *>(static_cast<char *>(a.v_pool) + at * ES) = x;
-        }
-    } else {
-        // four slots and 2 x 2 dims to a thread: a quad of slots that are all new makes two units, others go by 16 bits
-        constexpr int VT = D;                         // threads that a head's values take
-        const int vt = tid % VT, j = vt & 7, i32 = (vt >> 3) % (D / 32), quad = vt / (D / 4);
-        const int t0 = sub * 16 + 4 * quad, d0 = 32 * i32 + 2 * j;
-        if (t0 + 4 <= t_lo || t0 >= t_hi) return;
-        for (int g = g0 + tid / VT; g < g1; g += THREADS / VT) {
-            uint32_t lo2[4], hi2[4];                  // [slot]: dims d0, d0 + 1 and d0 + 16, d0 + 17
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {             // (slots that are not new: the nearest that is)
-                const size_t row = (size_t)first + (min(max(t0 + e, t_lo), t_hi - 1) - p0);
-                const char *x = v + (row * a.v_stride + (size_t)g * D + d0) * 2;
-                lo2[e] = *reinterpret_cast<const uint32_t *>(x);
-                hi2[e] = *reinterpret_cast<const uint32_t *>(x + 32);
-            }
-            uint16_t *dst = static_cast<uint16_t *>(a.v_pool) + (((size_t)block * a.num_layers + a.layer) * Hkv + g) * tile + sub_at + (size_t)((i32 * 4 + quad) * 16 + 2 * j) * 8;
-            if (t0 >= t_lo && t0 + 4 <= t_hi) {
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int sh = 16 * e;
-                    uint4 u;
-                    u.x = ((lo2[0] >> sh) & 0xFFFFu) | ((lo2[1] >> sh) << 16);
-                    u.y = ((lo2[2] >> sh) & 0xFFFFu) | ((lo2[3] >> sh) << 16);
-                    u.z = ((hi2[0] >> sh) & 0xFFFFu) | ((hi2[1] >> sh) << 16);
-                    u.w = ((hi2[2] >> sh) & 0xFFFFu) | ((hi2[3] >> sh) << 16);
-                    *reinterpret_cast<uint4 *>(dst + e * 8) = u;
-                }
+                if (live) *reinterpret_cast<uint4 *>(static_cast<char *>(a.k_pool) + (at + o) * ES) = z;
             } else {
-#pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    if (t0 + s < t_lo || t0 + s >= t_hi) continue;
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        dst[e * 8 + s] = (uint16_t)(lo2[s] >> (16 * e));
-                        dst[e * 8 + 4 + s] = (uint16_t)(hi2[s] >> (16 * e));
-                    }
-                }
+                put_values(x[u], g0 + i - nk);
             }
         }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) x[u] = y[u];
     }
 }
 
