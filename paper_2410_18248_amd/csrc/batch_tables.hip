@@ -7,10 +7,12 @@
 // behind that one counts any: so the rows of those served follow each other.
 //
 // Bound by the launch and the round trips: lengths, the sums, ids (and kept entries), stores.  One launch: every workgroup sums the
-// whole batch up for itself, which is a load per request of a thread and two scans, and then writes its own part of the table
-// (2 048 entries) or of the slots (1 024); the first one writes lengths and first rows.  A second launch behind one that sums
+// whole batch up for itself, which is a load per request of a thread and two scans, keeps what its own part asks for in LDS, and writes that part:
+// 2 048 entries of the table, a request's whole row at most, or 1 024 slots; the first one writes lengths and first rows.  A second launch behind one that sums
 // costs more than the sums do.
 #include <hip/hip_runtime.h>
+
+#include <algorithm>
 
 #include "attn_reducers.h"
 #include "internal.h"
@@ -66,17 +68,30 @@ __device__ __forceinline__ Lengths lengths_of(const TableArgs &a, int r)
     return x;
 }
 
-// K requests per thread, in order.  Dynamic LDS: ids before each request, then rows before each request and behind the last; bit 31 of
-// the former: not served.
+// What a part of the table or of the slots asks for of a request.
+struct Held {
+    int before, held, need;                           // first id, entries held, entries taken (-1: not served, the row is left alone)
+};
+
+// K requests per thread, in order.  Dynamic LDS: workgroups of the table, Held of the rows they write; of the slots, all requests' first rows and ids and
+// cached tokens.
 template <int K>
 __global__ __launch_bounds__(kTableThreads) void batch_tables(const TableArgs a)
 {
-    extern __shared__ uint32_t sums[];
+    extern __shared__ int kept[];
     __shared__ uint32_t waves[3][kTableThreads / 64];
     __shared__ int missing[2];                        // requests not served, the lowest
     __shared__ uint32_t taken;
-    const int tid = threadIdx.x, n = a.n_req;
-    uint32_t *ids_before = sums, *rows_before = sums + n;
+    const int tid = threadIdx.x, n = a.n_req, item = (int)blockIdx.x - 1;
+    // the part: rows r0 .. r1 of the table, from entry e0 (of r0's row) on
+    const bool lengths = item < 0, rows_part = !lengths && item < a.table_items;
+    int r0 = 0, r1 = -1, e0 = 0;
+    if (rows_part) {
+        const long long from = (long long)item * kTableEntries;
+        r0 = (int)(from / a.max_blocks);
+        e0 = (int)(from - (long long)r0 * a.max_blocks);
+        r1 = min(n - 1, r0 + (e0 + kTableEntries - 1) / a.max_blocks);
+    }
     Lengths x[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) x[k] = lengths_of(a, tid * K + k);
@@ -98,41 +113,79 @@ __global__ __launch_bounds__(kTableThreads) void batch_tables(const TableArgs a)
         if (tokens[k] != 0xffffffffu) mine = add_sat(mine, tokens[k]);
     }
     at = sum_before(mine, waves[1]);
-    uint32_t rows[K], most = 0;                       // rows in front of each; of all that are served
+    uint32_t first[K], most = 0;                      // rows in front of each; of all that are served
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        rows[k] = at;
+        first[k] = at;
         if (tokens[k] == 0xffffffffu) continue;
         at = add_sat(at, tokens[k]);
         if (at <= (uint32_t)a.total_tokens) most = at;
         else if (tokens[k] > 0) tokens[k] = 0xffffffffu;
+    }
+    if (rows_part) {
+        Held *own = reinterpret_cast<Held *>(kept);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int r = tid * K + k;
+            if (r >= r0 && r <= r1) own[r - r0] = Held{(int)before[k], x[k].held, tokens[k] != 0xffffffffu ? x[k].need : -1};
+        }
+        __syncthreads();
+        // four entries at a time; all that a thread writes is asked for before the first is stored
+        constexpr int TURNS = kTableEntries / (4 * kTableThreads);
+        int v[TURNS][4];
+        bool put[TURNS][4];
+#pragma unroll
+        for (int i = 0; i < TURNS; ++i) {
+            const unsigned at0 = (unsigned)e0 + 4 * (i * kTableThreads + tid);     // entries behind the start of r0's row (below 2^27)
+            int r = (int)(at0 / (unsigned)a.max_blocks), col = (int)(at0 - (unsigned)r * (unsigned)a.max_blocks);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool in = r <= r1 - r0;
+                const Held h = own[in ? r : 0];
+                const int j = col - h.held;
+                put[i][e] = in && h.need >= 0 && j >= 0;
+                v[i][e] = put[i][e] && j < h.need ? a.block_ids[h.before + j] : -1;
+                if (++col == a.max_blocks) {
+                    col = 0;
+                    ++r;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < TURNS; ++i) {
+            int32_t *to = a.block_table + (long long)item * kTableEntries + 4 * (i * kTableThreads + tid);
+            if (put[i][0] && put[i][1] && put[i][2] && put[i][3] && a.wide) {
+                *reinterpret_cast<int4 *>(to) = make_int4(v[i][0], v[i][1], v[i][2], v[i][3]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (put[i][e]) to[e] = v[i][e];
+            }
+        }
+        return;
     }
     most = (uint32_t)wave_max_to((int)most);          // (no more than total_tokens: not negative)
     if ((tid & 63) == 63) waves[2][tid >> 6] = most;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kTableThreads / 64; ++w) most = max(most, waves[2][w]);
-    int lost = 0, lowest = 0x7fffffff;
-    uint32_t used = 0;
+    if (lengths) {
+        int lost = 0, lowest = 0x7fffffff;
+        uint32_t used = 0;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int r = tid * K + k;
-        if (r >= n) break;
-        const bool served = tokens[k] != 0xffffffffu;
-        ids_before[r] = served ? (x[k].need > 0 ? before[k] : 0u) : 0x80000000u;
-        rows_before[r] = min(rows[k], most);
-        if (served) used += (uint32_t)x[k].need;
-        else {
-            ++lost;
-            lowest = min(lowest, r);
-        }
-        if (blockIdx.x == 0) {
+        for (int k = 0; k < K; ++k) {
+            const int r = tid * K + k;
+            if (r >= n) break;
+            const bool served = tokens[k] != 0xffffffffu;
+            if (served) {
+                used += (uint32_t)x[k].need;
+            } else {
+                ++lost;
+                lowest = min(lowest, r);
+            }
             a.ctx_lens[r] = served ? x[k].cached + x[k].fresh : 0;
-            a.q_start[r] = (int)min(rows[k], most);
+            a.q_start[r] = (int)min(first[k], most);
         }
-    }
-    if (tid == 0) rows_before[n] = most;
-    if (blockIdx.x == 0) {
         if (tid == 0) a.q_start[n] = (int)most;
         if (a.report) {
             if (lost) {
@@ -150,67 +203,43 @@ __global__ __launch_bounds__(kTableThreads) void batch_tables(const TableArgs a)
         }
         return;
     }
+    // slots, four rows to a thread: the last request whose rows begin at or in front of the first (that one has some) is searched for, the others' follow it
+    int *starts = kept, *ids_before = starts + n + 1, *cached = ids_before + n;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int r = tid * K + k;
+        if (r < n) {
+            starts[r] = (int)min(first[k], most);
+            ids_before[r] = (int)before[k];
+            cached[r] = x[k].cached;
+        }
+    }
+    if (tid == 0) starts[n] = (int)most;
     __syncthreads();
-    const int item = blockIdx.x - 1;
-    if (item < a.table_items) {                       // a stretch of the table: four entries at a time
-        const long long all = (long long)n * a.max_blocks;
-        for (int i = 0; i < kTableEntries / (4 * kTableThreads); ++i) {
-            const long long e0 = (long long)item * kTableEntries + 4 * (i * kTableThreads + tid);
-            if (e0 >= all) break;
-            int r = (int)(e0 / a.max_blocks), col = (int)(e0 - (long long)r * a.max_blocks);
-            int v[4];
-            bool put[4];
-            int held = 0, need = 0, from = 0;
-            bool served = false;
-            const auto enter = [&]() {
-                const Lengths y = lengths_of(a, r);
-                served = !(ids_before[r] >> 31);
-                from = (int)(ids_before[r] & 0x7fffffffu);
-                held = y.held;
-                need = y.need;
-            };
-            enter();
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int j = col - held;
-                put[e] = e0 + e < all && served && j >= 0;
-                v[e] = put[e] && j < need ? a.block_ids[from + j] : -1;
-                if (++col == a.max_blocks && e < 3 && e0 + e + 1 < all) {
-                    col = 0;
-                    ++r;
-                    enter();
-                }
-            }
-            int32_t *to = a.block_table + e0;
-            if (put[0] && put[1] && put[2] && put[3] && a.wide) {
-                *reinterpret_cast<int4 *>(to) = make_int4(v[0], v[1], v[2], v[3]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (put[e]) to[e] = v[e];
-            }
-        }
-        return;
+    constexpr int TURNS = kTableSlots / kTableThreads;
+    const int row0 = (item - a.table_items) * kTableSlots + tid * TURNS;
+    if (row0 < 0 || row0 >= a.total_tokens) return;
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (starts[mid] <= row0) lo = mid; else hi = mid;
     }
-    const int n0 = (item - a.table_items) * kTableSlots;
+    const int round = (1 << a.log2_block_size) - 1;
+    int block[TURNS], slot[TURNS];
 #pragma unroll
-    for (int i = 0; i < kTableSlots / kTableThreads; ++i) {
-        const uint32_t row = (uint32_t)n0 + i * kTableThreads + tid;
-        if (row >= (uint32_t)a.total_tokens) break;
-        long long slot = -1;
-        if (row < most) {
-            int lo = 0, hi = n;                       // the last request whose rows begin at or in front of it: that one has some
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (rows_before[mid] <= row) lo = mid; else hi = mid;
-            }
-            const Lengths y = lengths_of(a, lo);
-            const int p = y.cached + (int)(row - rows_before[lo]), j = (p >> a.log2_block_size) - y.held;
-            const int block = j < 0 ? a.block_table[(size_t)lo * a.max_blocks + j + y.held] : a.block_ids[(ids_before[lo] & 0x7fffffffu) + j];
-            if ((unsigned)block < (unsigned)a.num_blocks) slot = ((long long)block << a.log2_block_size) + (p & ((1 << a.log2_block_size) - 1));
+    for (int i = 0; i < TURNS; ++i) {
+        block[i] = -1;
+        slot[i] = 0;
+        if ((uint32_t)row0 + i < most) {
+            while (starts[lo + 1] <= row0 + i) ++lo;  // (ends: the last start is `most`)
+            const int c = cached[lo], p = c + (row0 + i - starts[lo]), entry = p >> a.log2_block_size, held = a.grow ? (c + round) >> a.log2_block_size : 0;
+            slot[i] = p & round;
+            block[i] = entry < held ? a.block_table[(size_t)lo * a.max_blocks + entry] : a.block_ids[ids_before[lo] + entry - held];
         }
-        a.slots[row] = slot;
     }
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i)
+        if ((uint32_t)row0 + i < (uint32_t)a.total_tokens) a.slots[row0 + i] = (unsigned)block[i] < (unsigned)a.num_blocks ? ((long long)block[i] << a.log2_block_size) + slot[i] : -1;
 }
 
 }  // namespace
@@ -224,7 +253,8 @@ hipError_t launch_batch_tables(TableArgs a, hipStream_t stream)
     a.table_items = (int)items;
     a.wide = ((uintptr_t)a.block_table & 15) == 0;
     const dim3 grid((unsigned)(1 + items + slots)), block(kTableThreads);
-    const size_t lds = (2 * (size_t)a.n_req + 1) * sizeof(uint32_t);
+    const size_t rows = std::min((size_t)a.n_req, (size_t)kTableEntries / a.max_blocks + 2);
+    const size_t lds = std::max(a.slots ? (3 * (size_t)a.n_req + 1) * sizeof(int) : 0, rows * sizeof(Held));
     if (a.n_req <= kTableThreads)
         hipLaunchKernelGGL(batch_tables<1>, grid, block, lds, stream, a);
     else if (a.n_req <= 4 * kTableThreads)
