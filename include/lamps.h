@@ -341,8 +341,8 @@ int lamps_prefill_attn(lamps_ctx *ctx, int32_t layer, int32_t n_req, int32_t tot
  * counts are never read: such a block may have been given back (lamps_free_blocks)
  * and its entry hold anything.  The rest -- rows that do not run, empty contexts,
  * types, order, reproducibility, workspace -- is as for lamps_decode_attn, except
- * that a score, key or value that counts and is no finite number makes the row (or,
- * for a value, its element) no finite number either.
+ * that what counts and is no finite number does to a row what the equation says
+ * (NaN, or no weight for a score of minus infinity; a value of infinity may give NaN).
  *   q, out        device, [batch][H][d_h] dtype, 16-byte aligned
  * Errors: INVALID (null, alignment, window < 1, sinks < 0), RANGE (layer, batch). */
 int lamps_decode_attn_window(lamps_ctx *ctx, int32_t layer, int32_t batch, int32_t window,
@@ -461,8 +461,9 @@ int lamps_rope_append_tokens(lamps_ctx *ctx, int32_t layer, int32_t n_req, int32
  * if it brings tokens and these, counted in order, go beyond total_tokens.  Such a
  * request has length 0 and no rows, and its table row is not written.  The ids that it
  * would have taken stay with it: the next request begins behind them.
- * The outputs may overlap neither each other nor the inputs.
- * Errors: INVALID (null, overlap), RANGE (n_req > max_batch, negative sizes, n_ids >
+ * The outputs may overlap neither each other nor the inputs.  All arrays are aligned to
+ * their type.
+ * Errors: INVALID (null, alignment, overlap), RANGE (n_req > max_batch, negative sizes, n_ids >
  * num_blocks). */
 int lamps_batch_tables(lamps_ctx *ctx, int32_t n_req, int32_t total_tokens, const int32_t *cached,
                        const int32_t *new_tokens, const int32_t *block_ids, int32_t n_ids,

@@ -1026,6 +1026,9 @@ int lamps_batch_tables(lamps_ctx *c, int32_t n_req, int32_t total_tokens, const 
             return fail(c, LAMPS_ERR_RANGE, "lamps_batch_tables: n_req / total_tokens / n_ids out of range");
         if (n_ids > c->cfg.num_blocks)
             return fail(c, LAMPS_ERR_RANGE, "lamps_batch_tables: more ids than the pool has blocks");
+        if ((((uintptr_t)cached | (uintptr_t)new_tokens | (uintptr_t)block_ids | (uintptr_t)block_table | (uintptr_t)ctx_lens | (uintptr_t)q_start |
+              (uintptr_t)report) & 3) || ((uintptr_t)slots & 7))
+            return fail(c, LAMPS_ERR_INVALID, "lamps_batch_tables: arrays must be aligned to their type");
         const size_t n = (size_t)n_req;
         const struct { const void *p; size_t bytes; } in[] = {{cached, n * 4}, {new_tokens, n * 4}, {block_ids, (size_t)n_ids * 4}},
             out[] = {{block_table, n * c->cfg.max_blocks_per_req * 4}, {ctx_lens, n * 4}, {q_start, (n + 1) * 4},

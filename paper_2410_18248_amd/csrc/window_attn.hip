@@ -422,12 +422,15 @@ long long most_positions(const WindowArgs &w, int unit)
     return std::min(row, (long long)w.window + w.sinks + 2 * unit);
 }
 
-// Parts of a range: as many as give every wave of the chip a walk, but two units to a wave at least, or the sum is longer than the walk.
+// Parts of a range: as many as give every wave of the chip a walk, but two units to a wave at least, or the sum is longer than the walk; none where a workgroup's own walk
+// is about as long as the way through a second launch (one request, window 256, 32 / 8 heads of 128: 5.9 us whole, 9.2 in two parts; 1 024 9.0 in eight parts,
+// 9.1 in four).
 template <typename R>
 int count_parts(const WindowArgs &w)
 {
     const DecodeArgs &a = w.d;
     const long long ranges = (long long)a.batch * a.num_kv_heads * a.passes, units = most_positions(w, R::U) / R::U;
+    if (units <= 9 * kWaves) return 1;
     const long long chip = 256LL * std::min(R::kMostPerCu, 4);
     const size_t state = (size_t)a.heads_per_pass * (a.head_dim + 2) * sizeof(float);
     long long parts = std::min(chip / ranges, units / (2 * kWaves));

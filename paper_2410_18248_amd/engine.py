@@ -8,6 +8,9 @@ Every iteration of Algorithm 1 (arXiv 2410.18248) becomes:
       recompute > 0 : lamps_alloc_blocks + lamps_kv_append_tokens + lamps_prefill_attn
                       per layer (Discard's recompute, a prompt, an API response)
       otherwise     : lamps_kv_append + lamps_decode_attn per layer (one new token)
+      both          : lamps_batch_tables for the batch's tables, from its lengths and blocks; for a
+                      model with rotary positions lamps_rope_append(_tokens) in place of the append,
+                      for layers with a window lamps_decode_attn_window / lamps_prefill_attn_window
   lamps_sched_commit(measured iteration time) -> who reached an API call and how it leaves
       Preserve: nothing;  Discard: lamps_free_blocks;
       Swap: lamps_swap_out to a pinned buffer, then lamps_free_blocks
@@ -21,7 +24,6 @@ the GEMMs are absent.  torch is plumbing: device memory, streams, the clock.
 """
 import time
 
-import numpy as np
 import torch
 
 from . import binding as P
@@ -67,14 +69,19 @@ class DeviceSource:
 
 
 class LiveEngine:
-    def __init__(self, cfg, sched_cfg, source, device="cuda:0", observer=None, layered_swap=False):
+    def __init__(self, cfg, sched_cfg, source, device="cuda:0", observer=None, layered_swap=False, rope=None, windows=None):
         """cfg: LampsConfig (pools are allocated here); sched_cfg: LampsSchedConfig whose
         memory_tokens must not exceed num_blocks * block_size; observer(kind, rid, layer, first_pos,
         out_rows): called with the attention output of every processed token (tests);
         layered_swap: swap layer-major, so that a returning request's first layers run while the
-        later ones are still on their way."""
+        later ones are still on their way;
+        rope: a LampsRope, by which queries and keys are normalised and turned on their way (default:
+        they are used as the source gives them);
+        windows: per layer None or (window, sinks), what a new token sees (default: everything)."""
         self.cfg, self.dev, self.source, self.observer = cfg, torch.device(device), source, observer
         self.layered = layered_swap
+        self.rope, self.windows = rope, windows or [None] * cfg.num_layers
+        assert len(self.windows) == cfg.num_layers
         self.tdtype = torch.bfloat16 if cfg.dtype == P.LAMPS_BF16 else torch.float32
         elems = P.lamps_pool_bytes(cfg) // (2 if cfg.dtype == P.LAMPS_BF16 else 4)
         self.k_pool = torch.zeros(elems, dtype=self.tdtype, device=self.dev)
@@ -114,11 +121,29 @@ class LiveEngine:
             self.lam.compute_wait_blocks(new)       # they may still be the source of a swap-out
             self.blocks[rid] += new
 
-    def _tables(self, rids):
-        t = np.full((len(rids), self.cfg.max_blocks_per_req), -1, dtype=np.int32)
-        for i, r in enumerate(rids):
-            t[i, :len(self.blocks[r])] = self.blocks[r]
-        return torch.from_numpy(t).to(self.dev, non_blocking=True)
+    def _batch(self, rids, cached, counts):
+        """The batch's table, lengths before and after its new tokens, and first rows, made on the device."""
+        bs, row, n = self.cfg.block_size, self.cfg.max_blocks_per_req, len(rids)
+        ids = [b for r, c, k in zip(rids, cached, counts) for b in self.blocks[r][:(c + k + bs - 1) // bs]]
+        given = torch.tensor(list(cached) + list(counts) + ids, dtype=torch.int32).to(self.dev)
+        made = torch.empty(n * (row + 2) + 1, dtype=torch.int32, device=self.dev)
+        table, after, start = made[:n * row].view(n, row), made[n * row:n * (row + 1)], made[n * (row + 1):]
+        self.lam.batch_tables(n, sum(counts), given[:n], given[n:2 * n], given[2 * n:], len(ids), False, table, after, start)
+        return table, given[:n], after, start
+
+    def _append(self, layer, q, k, v, n, table, lengths, running=None, start=None):
+        """Keys and values into the cache; returns the queries to attend with."""
+        lam, rope = self.lam, self.rope
+        if rope is None:
+            if start is None:
+                lam.kv_append(layer, n, k, v, table, lengths, running, False)
+            else:
+                lam.kv_append_tokens(layer, n, q.shape[0], k, v, start, table, lengths)
+        elif start is None:
+            lam.rope_append(layer, n, rope, q, k, v, table, lengths, running, False, q)
+        else:
+            lam.rope_append_tokens(layer, n, q.shape[0], rope, q, k, v, start, table, lengths, q)
+        return q
 
     def _release(self, rid):
         if self.blocks[rid]:
@@ -166,9 +191,7 @@ class LiveEngine:
                     self._grow(r, n)
                     self.ctx[r] += n
                 counts = [n for _, n in pre]
-                qs = torch.tensor(np.concatenate([[0], np.cumsum(counts)]), dtype=torch.int32, device=self.dev)
-                td = self._tables(rids)
-                cd = torch.tensor([self.ctx[r] for r in rids], dtype=torch.int32, device=self.dev)
+                td, _, cd, qs = self._batch(rids, first, counts)
                 total = int(sum(counts))
                 for layer in range(L):
                     for ticket in landing:
@@ -178,8 +201,12 @@ class LiveEngine:
                     k = torch.cat([p[1] for p in parts]).contiguous().to(self.dev)
                     v = torch.cat([p[2] for p in parts]).contiguous().to(self.dev)
                     out = torch.empty_like(q)
-                    lam.kv_append_tokens(layer, len(rids), total, k, v, qs, td, cd)
-                    lam.prefill_attn(layer, len(rids), total, q, qs, td, cd, out, max_new_tokens=max(counts))
+                    q = self._append(layer, q, k, v, len(rids), td, cd, start=qs)
+                    if self.windows[layer]:
+                        lam.prefill_attn_window(layer, len(rids), total, *self.windows[layer], q, qs, td, cd, out,
+                                                max_new_tokens=max(counts))
+                    else:
+                        lam.prefill_attn(layer, len(rids), total, q, qs, td, cd, out, max_new_tokens=max(counts))
                     if self.observer:
                         o = out.float().cpu()
                         at = 0
@@ -190,8 +217,7 @@ class LiveEngine:
             if dec:                                 # one new token per request
                 for r in dec:
                     self._grow(r, 1)
-                td = self._tables(dec)
-                cd = torch.tensor([self.ctx[r] for r in dec], dtype=torch.int32, device=self.dev)
+                td, cd, grown, _ = self._batch(dec, [self.ctx[r] for r in dec], [1] * len(dec))
                 md = torch.ones(len(dec), dtype=torch.uint8, device=self.dev)
                 for layer in range(L):
                     for ticket in landing:
@@ -202,9 +228,11 @@ class LiveEngine:
                     v = torch.cat([p[2] for p in parts]).contiguous().to(self.dev)
                     out = torch.empty_like(q)
                     # the new token's key and value go in first and attention sees them: lengths + 1
-                    # (on the last layer the append has already advanced the device lengths)
-                    lam.kv_append(layer, len(dec), k, v, td, cd, md, layer == L - 1)
-                    lam.decode_attn(layer, len(dec), q, td, cd if layer == L - 1 else cd + 1, md, out)
+                    q = self._append(layer, q, k, v, len(dec), td, cd, running=md)
+                    if self.windows[layer]:
+                        lam.decode_attn_window(layer, len(dec), *self.windows[layer], q, td, grown, md, out)
+                    else:
+                        lam.decode_attn(layer, len(dec), q, td, grown, md, out)
                     if self.observer:
                         o = out.float().cpu()
                         for i, r in enumerate(dec):

@@ -43,6 +43,9 @@ def main():
     ap.add_argument("--source", default="device", choices=["device", "host"],
                     help="where the random q / k / v rows are made (host: slow, the tests' source)")
     ap.add_argument("--layered-swap", action="store_true", help="swap layer-major (a returning request runs layer by layer)")
+    ap.add_argument("--rotary", action="store_true", help="queries and keys are normalised and turned on their way (rotary positions)")
+    ap.add_argument("--window", type=int, default=0, help="every other layer sees only the last WINDOW positions and the first --sinks")
+    ap.add_argument("--sinks", type=int, default=4)
     a = ap.parse_args()
     import torch
     pol = {"fcfs": P.LAMPS_POLICY_FCFS, "sjf": P.LAMPS_POLICY_SJF, "sjf_total": P.LAMPS_POLICY_SJF_TOTAL,
@@ -55,7 +58,13 @@ def main():
     cost = P.LampsCostModel(2e-3, 2e-8 * a.layers, 1e-3, 3e-6 * a.layers, 3e-4, 3.7e-7 * a.layers, 0, 0)
     scfg = P.LampsSchedConfig(pol, a.max_batch, a.memory_tokens, 100, 1, 2048, 0.5 * a.memory_tokens, M, cost)
     make = DeviceSource if a.source == "device" else RandomSource
-    eng = LiveEngine(cfg, scfg, make(a.seed, a.heads, a.kv_heads, D, torch.bfloat16), layered_swap=a.layered_swap)
+    rope = None
+    if a.rotary:
+        f = torch.tensor(P.lamps_rope_frequencies(D, 10000.0), dtype=torch.float64, device="cuda:0")
+        rope = P.LampsRope(D, frequencies=f, normalise=True)
+    windows = [(a.window, a.sinks) if a.window and layer % 2 == 0 else None for layer in range(a.layers)]
+    eng = LiveEngine(cfg, scfg, make(a.seed, a.heads, a.kv_heads, D, torch.bfloat16), layered_swap=a.layered_swap, rope=rope,
+                     windows=windows)
     trace = synthetic_trace(a.seed, a.requests, a.rate)
     for rid, arr, prompt, segs, _ in trace:
         eng.add(rid, arr, prompt, [(n, None if d is None else d * a.time_scale, rho, None) for n, d, rho in segs])

@@ -59,6 +59,7 @@ FORMS = [
     ("bf16", 4, 4, 128, 16, 48, 0, True, 2), ("bf16", 6, 2, 64, 16, 64, 0, True, 3), ("bf16", 8, 8, 64, 64, 16, 1, False, 0),
     ("bf16", 16, 1, 256, 16, 256, 0, True, 0), ("bf16", 2, 2, 256, 16, 80, 1, True, 1), ("bf16", 3, 3, 64, 16, 0, 0, True, 0),
     ("bf16", 8, 2, 128, 16, 0, 0, False, 0), ("f32", 4, 4, 64, 16, 64, 0, True, 0), ("f32", 8, 2, 32, 16, 32, 1, True, 3),
+    ("bf16", 40, 40, 128, 16, 128, 0, True, 0),                          # more than a workgroup's threads have in one turn
     ("f32", 3, 1, 128, 32, 128, 0, False, 1), ("f32", 2, 2, 128, 16, 112, 1, True, 2), ("f32", 5, 5, 32, 16, 16, 0, True, 0),
 ]
 

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import lamps_workloads as W
+import paper_2410_18248_amd as P
 from operator_forms import f64, seen, window_attn
 from rig import Rig, n2t, to_f64
 
@@ -128,10 +129,15 @@ def test_prefill(dtype, H, Hkv, D, bs, reqs, looks, rows):
         got = to_f64(out)
         assert (got[total:] == 2.5).all()
         for r, (c, n) in enumerate(reqs):
+            # (of long prompts the first and the last of 100 rows and some between, and all of the last tile)
+            pick = [i for i in range(n) if n <= 300 or i % 100 in (0, 41, 99) or n - i < 20]
             if n:
-                ref, size = window_attn(f64(q[start[r]:start[r + 1]]), f64(K[r]), f64(V[r]), c - n, window, sinks)
-                off = np.abs(got[start[r]:start[r + 1]] - ref) - bound(dtype, ref, size, not rows)
-                assert (off <= 0).all(), (window, sinks, r, c, n, off.max())
+                kd, vd = f64(K[r]), f64(V[r])
+                for i in pick:
+                    at = start[r] + i
+                    ref, size = window_attn(f64(q[at:at + 1]), kd, vd, c - n + i, window, sinks)
+                    off = np.abs(got[at] - ref[0]) - bound(dtype, ref[0], size[0], not rows)
+                    assert (off <= 0).all(), (window, sinks, r, c, n, i, off.max())
         rig.close()
 
 
@@ -200,6 +206,25 @@ def test_long_contexts_in_parts(dtype, H, Hkv, D, bs, layers, batch):
         ref, size = window_attn(f64(q[r:r + 1]), f64(K[r]), f64(V[r]), ctx[r] - 1, window, sinks)
         assert (np.abs(to_f64(out)[r] - ref[0]) <= bound(dtype, ref[0], size[0], False)).all()
     rig.close()
+
+
+def test_lengths_beyond_the_row_are_clamped():
+    for dtype, H, Hkv, D in [("bf16", 8, 2, 128), ("bf16", 4, 4, 64), ("f32", 4, 2, 32)]:
+        geom, rig, table, K, V, ctx = _setup(dtype, H, Hkv, D, 16, [(64, 1), (64, 1), (30, 1)], 20, 2, 4)
+        full = np.ascontiguousarray(table[:, :4])                        # (a row of 64 positions, all of them there)
+        rig.lamps.destroy()
+        cfg = P.LampsConfig(2, H, Hkv, D, 16, geom.num_blocks, 4, 3, rig.cfg.dtype)
+        rig.lamps = P.Lamps(cfg, rig.k_pool, rig.v_pool, rig.workspace)
+        q = n2t(W.queries(1, geom, 3), rig.dev)
+        outs = []
+        for lens in ([64, 64, 30], [65, 2 ** 31 - 1, 30], [64, 64, -1]):
+            out = torch.full((3, H, D), 2.5, dtype=rig.tdtype, device=rig.dev)
+            rig.lamps.decode_attn_window(1, 3, 20, 2, q, torch.as_tensor(full, device=rig.dev), torch.tensor(lens, dtype=torch.int32, device=rig.dev),
+                                         torch.ones(3, dtype=torch.uint8, device=rig.dev), out)
+            torch.cuda.synchronize()
+            outs.append(out)
+        assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0][:2], outs[2][:2]) and bool((outs[2][2] == 0).all())
+        rig.close()
 
 
 def test_bad_lengths_and_entries_are_harmless():

@@ -90,6 +90,7 @@ def test_tables_refuse(lam):
             (dict(cached=0), -1, "null"), (dict(new=0), -1, "null"), (dict(ids=0), -1, "null"), (dict(table=0), -1, "null"), (dict(lens=0), -1, "null"),
             (dict(start=0), -1, "null"), (dict(lens=A), -1, "overlaps"), (dict(lens=A + 8), -1, "overlaps"), (dict(start=2 * A - 4), -1, "overlaps"),
             (dict(table=3 * A - 4), -1, "overlaps"), (dict(slots=4 * A + 8), -1, "overlap"), (dict(report=7 * A), -1, "overlap"),
+            (dict(slots=7 * A + 4), -1, "aligned"), (dict(cached=A + 2), -1, "aligned"), (dict(report=8 * A + 1), -1, "aligned"),
             (dict(n=5), -2, "n_req"), (dict(n=-1), -2, "n_req"), (dict(total=-1), -2, "total"), (dict(n_ids=-1), -2, "n_ids"), (dict(n_ids=33), -2, "blocks")]:
         _refused(lambda: call(**kw), status, word)
 
