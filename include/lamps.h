@@ -415,7 +415,7 @@ int lamps_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, dou
  *   k_new, v_new   device, [batch] rows of [H_kv][d_h], k_stride / v_stride apart
  *                  (so that the three may be parts of one projection's rows; 0 => the
  *                  rows follow each other).  16-byte aligned, strides multiples of
- *                  16 bytes and no less than a row.
+ *                  16 bytes, no less than a row and no more than 2^28 elements.
  *   q_out          device, [batch][H][d_h], 16-byte aligned; may be q itself where
  *                  q's rows follow each other, and may not overlap the inputs otherwise
  * Errors: INVALID (null, alignment, strides, overlap, rope), RANGE (layer, batch). */

@@ -47,6 +47,12 @@ class LampsRope(ctypes.Structure):
 
     def __init__(self, rotary_dim, pairs=LAMPS_ROPE_HALVES, frequencies=None, amplitude=0.0, normalise=False, norm_eps=1e-6,
                  q_weight=None, k_weight=None):
+        if hasattr(frequencies, "element_size"):        # a tensor: the device reads rotary_dim / 2 doubles, one behind the other
+            if not (frequencies.is_floating_point() and frequencies.element_size() == 8 and frequencies.is_contiguous() and
+                    frequencies.numel() >= rotary_dim // 2):
+                raise LampsError(-1, "LampsRope: frequencies must be rotary_dim / 2 contiguous float64 numbers")
+        if any(hasattr(x, "is_contiguous") and not x.is_contiguous() for x in (q_weight, k_weight)):
+            raise LampsError(-1, "LampsRope: q_weight and k_weight must be contiguous")
         super().__init__(rotary_dim, pairs, 1 if normalise else 0, norm_eps, amplitude, _ptr(frequencies) or None,
                          _ptr(q_weight) or None, _ptr(k_weight) or None)
         self._keep = (frequencies, q_weight, k_weight)

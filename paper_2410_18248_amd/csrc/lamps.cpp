@@ -221,9 +221,9 @@ const char *fill_rope_args(lamps_ctx *c, lamps::RopeArgs *pa, int32_t layer, int
     if (q_stride == 0) q_stride = qrow;
     if (k_stride == 0) k_stride = krow;
     if (v_stride == 0) v_stride = krow;
-    const int64_t most = (int64_t)1 << 40;
-    if (q_stride < qrow || k_stride < krow || v_stride < krow || q_stride > most || k_stride > most || v_stride > most)
-        return "a stride is less than a row";
+    const int64_t most = (int64_t)1 << 28;                // (2^31 rows of 4-byte elements: 2^61 bytes, which 64 bits hold)
+    if (q_stride < qrow || k_stride < krow || v_stride < krow) return "a stride is less than a row";
+    if (q_stride > most || k_stride > most || v_stride > most) return "a stride is more than 2^28 elements";
     if (q_stride * es % 16 != 0 || k_stride * es % 16 != 0 || v_stride * es % 16 != 0) return "strides must be multiples of 16 bytes";
     if (rows > 0) {
         const size_t out = (size_t)rows * qrow * es;

@@ -4,6 +4,7 @@ import math
 
 import numpy as np
 import pytest
+import torch
 
 import paper_2410_18248_amd as P
 from test_boundary_cpu import _cfg
@@ -81,6 +82,29 @@ def test_rope_calls_refuse(lam):
     many(total=0)
     many(batch=0)
     assert lam.lib.lamps_rope_append(lam.h, 0, 1, None, A, 0, A, 0, A, 0, A, A, A, 0, 2 * A) == -1
+
+
+def test_rope_strides_beyond_what_64_bits_hold(lam):
+    # 2^30 rows of 2^40 elements: the end of such rows has no address, and rows of 2^28 elements that do not overlap must not seem to
+    rope = P.LampsRope(64, frequencies=A)
+    for at in range(3):
+        strides = [0, 0, 0]
+        strides[at] = 1 << 40
+        _refused(lambda: lam.rope_append_tokens(0, 2, 1 << 30, rope, A, 2 * A, 3 * A, A, A, A, 1 << 61, *strides), -1, "2^28")
+        _refused(lambda: lam.rope_append(0, 2, rope, A, 2 * A, 3 * A, A, A, A, False, 1 << 61, *strides), -1, "2^28")
+    _refused(lambda: lam.rope_append_tokens(2, 2, 1 << 30, rope, A, 2 * A, 3 * A, A, A, A, 1 << 61, 1 << 28, 1 << 28, 1 << 28), -2, "layer")
+    _refused(lambda: lam.rope_append_tokens(2, 2, 1 << 30, rope, A, 2 * A, 3 * A, A, A, A, 1 << 50, 1 << 28, 1 << 28, 1 << 28), -1, "overlaps")
+
+
+def test_rope_tensors_of_another_form_refuse():
+    f = torch.tensor(P.lamps_rope_frequencies(64, 10000.0), dtype=torch.float64)
+    P.LampsRope(64, frequencies=f)
+    P.LampsRope(32, frequencies=f)                  # (more than it reads)
+    for bad in (f.float(), f[:31], f.view(torch.int64), torch.stack([f, f], 1)[:, 0]):
+        _refused(lambda: P.LampsRope(64, frequencies=bad), -1, "float64")
+    w = torch.ones(128, 2)
+    for kw in (dict(q_weight=w[:, 0]), dict(k_weight=w[:, 1])):
+        _refused(lambda: P.LampsRope(64, frequencies=f, normalise=True, **kw), -1, "contiguous")
 
 
 def test_tables_refuse(lam):
