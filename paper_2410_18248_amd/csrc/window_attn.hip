@@ -300,8 +300,9 @@ __device__ __forceinline__ void put_out(void *out, size_t i, float inv, const fl
 // ---------------------------------------------------------------- one new token per request
 
 // A workgroup takes a range, one (request, kv head / pass), or one of the parts of it that the host has counted: its waves a stretch of the units each,
-// added up in LDS.  Parts leave their states to a second launch.  Bound by memory where the launch is large, otherwise by the round trips
-// of one walk: length, table entries, K / V, the sum.
+// added up in LDS.  Parts leave their states to a second launch.  Bound by memory where the launch is large (230 of 256 requests on 32 / 8 heads of 128, window 1 024:
+// 89 us, 5.7 TB/s; 51 of 64 on 32 plain heads, 2 048: 184 us, 5.9 TB/s), otherwise by the round trips
+// of one walk: length, table entries, K / V, the sum (one request, window 1 024: 5.6 us, and 3.1 of adding the parts up).
 template <typename R>
 __global__ __launch_bounds__(kThreads, R::kLeastPerCu) void window_decode(const WindowArgs w)
 {
@@ -530,11 +531,16 @@ template <int D>
 hipError_t launch_tiles_f32(WindowArgs w, hipStream_t s)
 {
     const int GH = f32_heads(w.d.num_q_heads / w.d.num_kv_heads), TW = 16 / GH;
-    const long long items = (long long)w.total_tokens / TW + w.d.batch, grid = (items * (w.d.num_q_heads / GH) + 7) / 8 * 8;
-    if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
+    const long long items = (long long)w.total_tokens / TW + w.d.batch, all = items * (w.d.num_q_heads / GH);
+    if (all > 0x7ffffff8LL) return hipErrorInvalidValue;
     w.items = (int)items;
     w.parts = 1;
-    hipLaunchKernelGGL(window_tiles_f32<D>, dim3((unsigned)grid), dim3(kThreads), 0, s, w);
+    // A tile to a wave where that keeps all of them at work and a walk is short, so that its latency is not what the launch takes (time over that of a tile to four
+    // waves: 5 600 tiles, 8 plain heads of 64, windows of 50 / 250 / 500 / 1 000 0.74 / 0.91 / 0.98 / 1.09, 32 / 8 heads of 128, 50 / 250 / 1 000, 0.76 / 0.89 /
+    // 1.01; 4 000 of 8 / 2 heads of 32, 50 / 250 / 1 000, 0.69 / 0.86 / 1.14; 2 100 of 64, 50 / 250, 0.97 / 1.13; 600, 1.2 to 1.5).
+    const bool alone = (w.total_tokens / TW) * (long long)(w.d.num_q_heads / GH) >= 3500 && most_positions(w, 16) <= 512 + 32;
+    if (alone) hipLaunchKernelGGL((window_tiles_f32<D, true>), dim3((unsigned)(((all + kWaves - 1) / kWaves + 7) / 8 * 8)), dim3(kThreads), 0, s, w);
+    else hipLaunchKernelGGL((window_tiles_f32<D, false>), dim3((unsigned)((all + 7) / 8 * 8)), dim3(kThreads), 0, s, w);
     return hipGetLastError();
 }
 

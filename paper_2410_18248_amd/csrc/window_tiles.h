@@ -5,11 +5,12 @@
 // prefill_mfma, whose products, operand layouts and lazily moved reference these are.  What differs is what a tile walks over: the units of 16
 // positions that any of its tokens sees -- of the sinks, then of the windows, which begin where the first token's does -- two units to a stage,
 // wherever they lie.  Units that all columns of a wave see need no mask; the others get one by position, and there a value that is no finite number must
-// not reach the columns that do not see it (a zero weight does not silence it): stages that hold one, which is found with two packed
-// operations per register, multiply once per token of the wave, with what that one does not see zeroed.
+// not reach the columns that do not see it (a zero weight does not silence it): stages that hold one, which is found by a product of the values
+// with zeros, multiply once per token of the wave, with what that one does not see zeroed.
 //
 // Bound by the matrix cores and the vector ALUs on long prompts, as prefill_mfma is, and by the walk where few tokens leave the chip idle: then
-// the stages of a tile are shared by `parts` workgroups, as many as the host counts from window and sinks, and a second launch adds them up.
+// the stages of a tile are shared by `parts` workgroups, as many as the host counts from window and sinks, and a second launch adds them up
+// (12 responses of 4 to 64 tokens on 32 / 8 heads, window 2 048: 36 us and 7).
 
 // Which workgroup does what: items -- tiles of one head, numbered by the row that they begin at, at most one for nothing per request -- head by
 // head, and of these an eighth, one after the other, to each of the eight XCDs: neighbours in time and place share most of their windows in an L2.
@@ -22,11 +23,10 @@ __device__ __forceinline__ int tile_item(const WindowArgs &w, unsigned block, in
     const unsigned all = (unsigned)w.items * (unsigned)heads * (unsigned)w.parts, per = (all + 7) / 8, i = (block & 7) * per + (block >> 3);
     return block >> 3 < per && i < all ? (int)i : -1;
 }
-__device__ __forceinline__ bool tile_at(const WindowArgs &w, int WT, TileAt &at, int heads)
+__device__ __forceinline__ bool tile_at(const WindowArgs &w, int WT, TileAt &at, int i0)
 {
     const DecodeArgs &a = w.d;
     const unsigned items = (unsigned)w.items;
-    const int i0 = tile_item(w, blockIdx.x, heads);
     if (i0 < 0) return false;
     const unsigned i = (unsigned)i0;
     // (uniform, and said to be: divisions go through the vector ALUs, and addresses of loads into LDS are scalars)
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : (tile_small<D, 
     const DecodeArgs &a = w.d;
     const int G = a.num_q_heads / a.num_kv_heads, TW = kCols / G, WT = kWaves * TW;
     TileAt at;
-    if (!tile_at(w, WT, at, a.num_kv_heads)) return;
+    if (!tile_at(w, WT, at, tile_item(w, blockIdx.x, a.num_kv_heads))) return;
     const int r = at.r, g = at.g, first = at.first, base_pos = at.ctx - at.n_new;
     const int n_new = min(at.n_new, w.total_tokens - first);
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -446,7 +446,7 @@ __global__ __launch_bounds__(kThreads) void window_join(const WindowArgs w0)
             for (int s = 0; s < 2; ++s) y[k][s] = *reinterpret_cast<const f32x4 *>(from + (size_t)block * 16 * D + (slab + s) * 256 + 4 * lane);
         }
         if (k0 == 0) {
-            on = tile_at(w, WT, at, a.num_kv_heads);
+            on = tile_at(w, WT, at, item);
             if (!on) return;
         }
 #pragma unroll
@@ -477,6 +477,9 @@ __global__ __launch_bounds__(kThreads) void window_join(const WindowArgs w0)
 // ---------------------------------------------------------------- two teams of waves
 
 // prefill_teams' way through a tile of 256 columns, for launches with many new tokens (grouped heads: plain ones are as fast or faster by window_tiles).
+// Bound by the two teams' phases in turn, matrix cores and vector ALUs; what a tile costs beyond its stages, its queries and outputs, two masked ends and the filling of
+// the pipeline, is 11 of 35 us under a window of 1 024: 4 prompts of 8 192 on 32 / 8 heads take 565 us, 915 TFLOP/s of the positions seen.  Tiles in
+// chains, the next one's first stages asked for behind the last one's, took 580 to 600.
 template <int D, int kCB>
 __global__ __launch_bounds__(512, 2) void window_teams(const WindowArgs w)
 {
@@ -493,7 +496,7 @@ __global__ __launch_bounds__(512, 2) void window_teams(const WindowArgs w)
     const DecodeArgs &a = w.d;
     const int G = a.num_q_heads / a.num_kv_heads, TW = kCols / G, WT = W * TW, window = w.window, sinks = w.sinks;
     TileAt at;
-    if (!tile_at(w, WT, at, a.num_kv_heads)) return;
+    if (!tile_at(w, WT, at, tile_item(w, blockIdx.x, a.num_kv_heads))) return;
     const int r = at.r, g = at.g, tile = at.tile, first = at.first, n_new = min(at.n_new, w.total_tokens - first), C = at.ctx - at.n_new + n_new;
 #include "teams_body.h"
 }

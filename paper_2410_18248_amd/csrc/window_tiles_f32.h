@@ -4,7 +4,8 @@
 // One workgroup = one (request, heads of a pass, tile of new tokens): 16 columns, (new token, head) pairs of one kv head, as in prefill_tiles_f32, whose
 // operands and sums (MfmaF32Tile) these are; its four waves take every fourth of the units that the tile's tokens see and add their states up in LDS.
 // Units that some column does not see whole are masked, and values there that are no finite numbers kept from the columns that do not see them.
-// Bound by the walk on short prompts, by the fp32 matrix rate on long ones.
+// In large launches with short walks a wave has a tile of its own.
+// Bound by the walk on short prompts (6 of 17 to 700 tokens, 8 heads of 64, window 100: 17 us, of which the matrix rate is 4), by the fp32 matrix rate on long ones.
 template <int DIM>
 struct WindowF32Tile : MfmaF32Tile<DIM> {
     typedef MfmaF32Tile<DIM> Base;
@@ -168,26 +169,44 @@ __host__ __device__ __forceinline__ int f32_heads(int group)
     return gh;
 }
 
-template <int D>
+// ALONE: a wave has a tile of its own, and no sum to make.
+template <int D, bool ALONE>
 __global__ __launch_bounds__(kThreads, D == 128 ? 2 : 1) void window_tiles_f32(const WindowArgs w)
 {
     typedef WindowF32Tile<D> R;
     constexpr int ROW = D + 4;                        // floats; 16-byte aligned, rows in different banks
-    __shared__ __align__(16) float part[kWaves][16][ROW];
-    __shared__ float2 stat[kWaves][16];
     const DecodeArgs &a = w.d;
     const int G = a.num_q_heads / a.num_kv_heads, GH = f32_heads(G), passes = G / GH, TW = 16 / GH;
-    TileAt at;
-    if (!tile_at(w, TW, at, a.num_kv_heads * passes)) return;
-    const int g = at.g / passes, h0 = at.g * GH, base_pos = at.ctx - at.n_new, n_new = min(at.n_new, w.total_tokens - at.first);
     const int lane = threadIdx.x & 63, j = lane & 15, qd = lane >> 4, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    TileAt at;
+    const unsigned all = (unsigned)w.items * (unsigned)(a.num_kv_heads * passes), per = ((all + kWaves - 1) / kWaves + 7) / 8;   // ALONE: workgroups to an XCD
+    const unsigned mine = ((blockIdx.x & 7) * per + (blockIdx.x >> 3)) * kWaves + wv;
+    if (!tile_at(w, TW, at, !ALONE ? tile_item(w, blockIdx.x, a.num_kv_heads * passes) : blockIdx.x >> 3 < per && mine < all ? (int)mine : -1)) return;
+    const int g = at.g / passes, h0 = at.g * GH, base_pos = at.ctx - at.n_new, n_new = min(at.n_new, w.total_tokens - at.first);
     const int toks = min(TW, n_new - at.tile * TW), tok = j / GH;   // this lane's column: token tile * TW + tok, head h0 + j % GH
     const bool ok = tok < toks;
     const int p_first = base_pos + at.tile * TW, p_last = p_first + toks - 1;
     const float *q = static_cast<const float *>(a.q) + ((size_t)(at.first + at.tile * TW + tok) * a.num_q_heads + h0 + j % GH) * D;
     const Sight<16> see(p_last + 1, max(0, p_first - w.window + 1), w.sinks, std::true_type{});
     typename R::State st;
-    R::reduce(a, at.r, g, ok ? q : nullptr, ok ? p_first + tok : -1, p_first, p_last, w.window, w.sinks, see, wv, kWaves, st);
+    R::reduce(a, at.r, g, ok ? q : nullptr, ok ? p_first + tok : -1, p_first, p_last, w.window, w.sinks, see, ALONE ? 0 : wv, ALONE ? 1 : kWaves, st);
+    if constexpr (ALONE) {
+        if (!ok) return;
+        const float inv = 1.0f / st.l;
+        float *out = static_cast<float *>(a.out) + (q - static_cast<const float *>(a.q));
+#pragma unroll
+        for (int c = 0; c < R::NC; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                typename R::vvec x;
+#pragma unroll
+                for (int v = 0; v < R::VW; ++v) x[v] = st.o[c][v][e] * inv;
+                *reinterpret_cast<typename R::vvec *>(out + 16 * R::VW * c + R::VW * (4 * qd + e)) = x;
+            }
+        return;
+    }
+    __shared__ __align__(16) float part[kWaves][16][ROW];
+    __shared__ float2 stat[kWaves][16];
     if (qd == 0) stat[wv][j] = make_float2(st.m, st.l);
 #pragma unroll
     for (int c = 0; c < R::NC; ++c)

@@ -250,3 +250,47 @@ def test_bad_lengths_and_entries_are_harmless():
         _prefill(rig, 1, q, reqs, wild, 40, 2, out, 0)
         assert torch.equal(out[:start[1]], good[:start[1]]) and torch.equal(out[start[2]:], good[start[2]:])
         rig.close()
+
+
+#          many tiles of 32-bit values under short windows: a tile to a wave
+WAVES = [
+    ("f32", 8, 2, 32, 16, [(3000, 3000), (2500, 2403), (5, 0), (1900, 1797), (20, 0)], [(33, 3), (490, 20)]),
+    ("f32", 32, 8, 128, 32, [(1000, 1000), (900, 801), (31, 31)], [(17, 2), (300, 5)]),
+    ("f32", 8, 8, 64, 16, [(4000, 4000), (3500, 3141)], [(100, 0)]),
+]
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,D,bs,reqs,looks", WAVES)
+def test_prefill_of_many_tiles(dtype, H, Hkv, D, bs, reqs, looks):
+    test_prefill(dtype, H, Hkv, D, bs, reqs, looks, False)
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,D,reqs,window,at", [
+    ("bf16", 16, 8, 128, [(2500, 2500), (2300, 2003)], 1030, (1000, 700)),       # two teams of waves
+    ("bf16", 8, 2, 128, [(900, 20), (700, 9)], 600, (895, 100)),                 # tiles in parts
+    ("bf16", 4, 4, 64, [(900, 20), (700, 9)], 600, (300, 695)),
+    ("f32", 32, 8, 128, [(1000, 1000), (900, 850)], 40, (500, 899)),             # a tile to a wave
+    ("f32", 8, 2, 32, [(4000, 4000), (3500, 3300)], 100, (1, 3411)),
+])
+def test_values_and_keys_that_are_no_numbers_in_large_and_shared_launches(dtype, H, Hkv, D, reqs, window, at):
+    """As test_what_a_token_does_not_see_has_no_part_in_its_row, one position of each request."""
+    sinks = 3
+    geom, rig, table, K, V, ctx = _setup(dtype, H, Hkv, D, 16, reqs, window, sinks, 6, clean=False)
+    total = sum(n for _, n in reqs)
+    q = W.queries(4, geom, total)
+    clean = torch.zeros((total, H, D), dtype=rig.tdtype, device=rig.dev)
+    _prefill(rig, 1, q, reqs, table, window, sinks, clean, 0)
+    for keys in (True, False):
+        Kb, Vb = [k.copy() for k in K], [v.copy() for v in V]
+        for r, p in enumerate(at):
+            (Kb if keys else Vb)[r][p] = 0x7FC0 if dtype == "bf16" else np.nan
+        rig.page_requests(1, table, Kb, Vb)
+        out = torch.zeros_like(clean)
+        start = _prefill(rig, 1, q, reqs, table, window, sinks, out, 0)
+        for r, (c, n) in enumerate(reqs):
+            sees = np.array([seen(p, c, window, sinks)[at[r]] for p in range(c - n, c)])
+            a, b = clean[start[r]:start[r + 1]].cpu(), out[start[r]:start[r + 1]].cpu()
+            assert sees.any()
+            assert torch.equal(a[~sees], b[~sees]), (keys, r)
+            assert not torch.isfinite(b[sees]).any(), (keys, r)
+    rig.close()
