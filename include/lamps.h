@@ -373,7 +373,8 @@ typedef enum { LAMPS_ROPE_HALVES = 0, LAMPS_ROPE_NEIGHBOURS = 1 } lamps_rope_pai
  *   then for every pair (a, b), the i-th,   with  u = p * frequencies[i]
  *       (a, b) <- amplitude * (a cos u - b sin u,  a sin u + b cos u)
  * in fp32 (the angle in fp64, so far positions keep their accuracy), rounded once
- * at the end.  Dims from rotary_dim on are not turned. */
+ * at the end.  Dims from rotary_dim on are not turned.  (The sum of a head's squares is one
+ * in fp32 as well: beyond 3.4e38 the head comes out as zeros.) */
 typedef struct {
     int32_t rotary_dim;         /* 0 (no rotation) .. head_dim, a multiple of 16      */
     int32_t pairs;              /* lamps_rope_pairs                                   */

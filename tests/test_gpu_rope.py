@@ -221,3 +221,39 @@ def test_infinities_stay_where_they_are():
     bad = ~torch.isfinite(out[0]).cpu()
     assert bad.nonzero().tolist() == [[1, 3], [1, 19], [2, 40]] and out[0, 2, 40] == float("-inf")
     rig.close()
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,D", [("bf16", 8, 2, 128), ("f32", 4, 4, 64)])
+def test_positions_at_the_end_of_the_longest_row(dtype, H, Hkv, D):
+    """A row of 2^30 positions.  On top of the bound above: an angle of 2^30 radians is rounded to 2^-24 here and by the kernel, which takes
+    2^27.4 turns off it, rounded to 2^-26 of a turn (1e-7 radians), by 1 / (2 pi), off by half a step (1.2e-7): 4e-7 together."""
+    bs, row = 64, 1 << 24
+    new, p0 = 37, (1 << 30) - 37
+    blocks = {p // bs for p in range(p0, p0 + new)} | {(1 << 29) // bs}
+    geom, rig, table = _rig(dtype, H, Hkv, D, bs, [blocks], row, 23, layers=1)
+    dev, rope = rig.dev, Rope(geom, rig.dev, D, 0, True, 0)
+    td = torch.as_tensor(table, device=dev)
+    far = lambda x: (np.abs(x[0]) <= bound(dtype, x[1], x[2]) + 4e-7 * x[2]).all()
+    (q, k, v), (qd, kd, vd), _ = _vectors(geom, dev, new, False, 5)
+    out = torch.zeros((new, H, D), dtype=rig.tdtype, device=dev)
+    torch.cuda.synchronize()
+    rig.lamps.rope_append_tokens(0, 1, new, rope.args, qd, kd, vd, torch.tensor([0, new], dtype=torch.int32, device=dev), td,
+                                 torch.tensor([1 << 30], dtype=torch.int32, device=dev), out)
+    one = torch.zeros((1, H, D), dtype=rig.tdtype, device=dev)
+    torch.cuda.synchronize()
+    rig.lamps.rope_append(0, 1, rope.args, qd, kd, vd, td, torch.tensor([(1 << 29) + 7], dtype=torch.int32, device=dev),
+                          torch.ones(1, dtype=torch.uint8, device=dev), False, one)
+    torch.cuda.synchronize()
+    p = np.arange(p0, p0 + new)
+    want, size = rope(q, p, 0)
+    assert far((to_f64(out) - want, want, size))
+    want, size = rope(q[:1], np.array([(1 << 29) + 7]), 0)
+    assert far((to_f64(one) - want, want, size))
+    kp, vp = t2n(rig.k_pool), t2n(rig.v_pool)
+    places = [(i, x) for i, x in enumerate(p)]
+    want, size = rope(k, p, 1)
+    for i, x in places:
+        at = table[0, x // bs], 0
+        assert far((f64(kp[at][:, rig.k_index[x % bs]]) - want[i], want[i], size[i])), i
+        assert (vp[at][:, rig.v_index[x % bs]] == v[i]).all(), i
+    rig.close()
