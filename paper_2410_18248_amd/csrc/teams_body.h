@@ -284,13 +284,15 @@
     auto buffer = [&](int st) { return lds + (st & (NB - 1)) * STAGE; };
     // WINDOW, values of stage st in registers, of which a column does not see all: if one of them is no finite number (which gives NaN times
     // zero), they are multiplied token by token, what that one does not see zeroed, and then taken away.
-    auto apart = [&](int st) {
+    // (all of them, or half at a time)
+    constexpr int APART = D <= 128 ? NS : NS / 2;
+    auto apart = [&](int st, int s0) {
         if (!masked(st)) return;
         const int t0 = unit(st, 0), t1 = unit(st, 1);
         f32x4 z = {0.f, 0.f, 0.f, 0.f};
         const bf16x8 zero = __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0));
 #pragma unroll
-        for (int s = 0; s < NS; ++s) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop[s], zero, z, 0, 0, 0);
+        for (int s = s0; s < s0 + APART; ++s) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop[s], zero, z, 0, 0, 0);
         if (!__any((z[0] + z[1]) + (z[2] + z[3]) != 0.0f)) return;
 #pragma unroll 1
         for (int tok = 0; tok < TW; ++tok) {
@@ -300,7 +302,7 @@
             for (int k = 0; k < 4; ++k)
                 keep[k] = (visible(p, k < 2 ? t0 : t1, 2 * (k & 1)) ? 0x0000FFFFu : 0u) | (visible(p, k < 2 ? t0 : t1, 2 * (k & 1) + 1) ? 0xFFFF0000u : 0u);
 #pragma unroll
-            for (int s = 0; s < NS; ++s) {
+            for (int s = s0; s < s0 + APART; ++s) {
                 uint4 u = __builtin_bit_cast(uint4, vop[s]);
                 u.x &= keep[0]; u.y &= keep[1]; u.z &= keep[2]; u.w &= keep[3];
 #pragma unroll
@@ -312,7 +314,7 @@
             }
         }
 #pragma unroll
-        for (int s = 0; s < NS; ++s) vop[s] = zero;
+        for (int s = s0; s < s0 + APART; ++s) vop[s] = zero;
     };
     // scores of stage st, outputs of stage st - 1; reads the values of st - 1 and the keys of st + 1
     auto matrix = [&](int st) {
@@ -329,10 +331,12 @@
             }
             pin();
         }
-        if constexpr (WINDOW) apart(st - 1);
+        if constexpr (WINDOW) apart(st - 1, 0);
         sums();
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
+            if constexpr (WINDOW && D > 128)
+                if (s == NS / 2) apart(st - 1, NS / 2);
             pv(s);
             if constexpr (D <= 128) {
                 read_k(kb, s >> 1, s & 1);
@@ -410,7 +414,8 @@
 #pragma unroll
     for (int s = 0; s < NS; ++s) read_v(buffer(wave_stages - 1), s);
     if constexpr (WINDOW) {
-        apart(wave_stages - 1);
+        apart(wave_stages - 1, 0);
+        if constexpr (D > 128) apart(wave_stages - 1, NS / 2);
     } else if (wave_stages * kStage > valid_end) {      // positions at or past the end carry no values
         const int v0 = valid_end - (wave_stages - 1) * kStage - 4 * qd, v1 = v0 - 16;
         const auto mask = [](int n) { return n >= 2 ? 0xFFFFFFFFu : n == 1 ? 0x0000FFFFu : 0u; };

@@ -516,7 +516,15 @@ hipError_t launch_tiles(const WindowArgs &w, hipStream_t s)
         if (G <= 32 && w.d.scale_log2e > 0.0f && walk >= 8 * WT && w.total_tokens >= 4LL * WT * w.d.batch && w.d.num_kv_heads * ((long long)w.total_tokens / WT) >= 256)
             return launch_teams<D, 2>(w, s);
     }
-    if constexpr (D >= 256) {                         // (as in prefill_mfma)
+    if constexpr (D >= 256) {
+        if constexpr (TILED) {
+            // Two teams, but where so few tiles have so long a walk that workgroups would share one (time over that of tiles of 128 columns by window_tiles, 16 heads of 256 on
+            // 1 to 8: windows of 64, 256 and 1 024, prompts and chunks on cached tokens, 0.68 to 1.0, one of 1.11; 8 of 128 on 3 000, window 3 000, 1.09; plain
+            // heads, whose other tiles are of 64 columns, 0.84 to 1.16).
+            const int WT = 128 / G;
+            if (G <= 16 && w.d.scale_log2e > 0.0f && w.d.num_kv_heads * ((long long)w.total_tokens / WT) * 16 >= walk) return launch_teams<D, 1>(w, s);
+        }
+        // (as in prefill_mfma)
         return launch_tiles<D, TILED, TILED ? 2 : 1>(w, s);
     } else {
         // Tiles of 64 columns, of which more fit a CU: where requests have few columns, and where a tile's own tokens are a large part of what it walks over (time over that

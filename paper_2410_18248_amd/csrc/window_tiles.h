@@ -476,7 +476,8 @@ __global__ __launch_bounds__(kThreads) void window_join(const WindowArgs w0)
 
 // ---------------------------------------------------------------- two teams of waves
 
-// prefill_teams' way through a tile of 256 columns, for launches with many new tokens (grouped heads: plain ones are as fast or faster by window_tiles).
+// prefill_teams' way through a tile of 256 columns (128 at head size 256), for launches with many new tokens (grouped heads: plain ones are as fast or faster by
+// window_tiles).
 // Bound by the two teams' phases in turn, matrix cores and vector ALUs; what a tile costs beyond its stages, its queries and outputs, two masked ends and the filling of
 // the pipeline, is 11 of 35 us under a window of 1 024: 4 prompts of 8 192 on 32 / 8 heads take 565 us, 915 TFLOP/s of the positions seen.  Tiles in
 // chains, the next one's first stages asked for behind the last one's, took 580 to 600.
@@ -490,7 +491,6 @@ __global__ __launch_bounds__(512, 2) void window_teams(const WindowArgs w)
     constexpr int NB = 131072 / STAGE;
     constexpr int VA = NB - 2, KA = NB == 4 ? NB : NB - 2;
     constexpr int NE = U / 256;
-    static_assert(D == 128, "a stage's values are all in registers before they are multiplied");
     extern __shared__ __align__(16) char lds[];
 
     const DecodeArgs &a = w.d;

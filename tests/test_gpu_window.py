@@ -294,3 +294,22 @@ def test_values_and_keys_that_are_no_numbers_in_large_and_shared_launches(dtype,
             assert torch.equal(a[~sees], b[~sees]), (keys, r)
             assert not torch.isfinite(b[sees]).any(), (keys, r)
     rig.close()
+
+
+#          heads of 256 in groups: two teams of waves, and tiles of 128 columns in parts
+TEAMS_256 = [
+    ("bf16", 4, 2, 256, 16, [(300, 300), (1, 1), (0, 0), (130, 50), (700, 41)], [(1, 0), (40, 3), (128, 33)]),
+    ("bf16", 16, 1, 256, 32, [(400, 90), (70, 70)], [(33, 0), (400, 7)]),
+    ("bf16", 6, 2, 256, 16, [(140, 140), (77, 10)], [(50, 4)]),                    # groups of 3
+    ("bf16", 16, 4, 256, 16, [(1500, 33), (900, 5)], [(64, 1), (1000, 4)]),
+]
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,D,bs,reqs,looks", TEAMS_256)
+def test_prefill_heads_of_256_in_groups(dtype, H, Hkv, D, bs, reqs, looks):
+    test_prefill(dtype, H, Hkv, D, bs, reqs, looks, False)
+
+
+@pytest.mark.parametrize("reqs,window,at", [([(300, 300), (200, 20)], 40, (100, 185)), ([(900, 20), (700, 9)], 600, (895, 100))])
+def test_values_and_keys_that_are_no_numbers_heads_of_256(reqs, window, at):
+    test_values_and_keys_that_are_no_numbers_in_large_and_shared_launches("bf16", 8, 4, 256, reqs, window, at)
