@@ -102,6 +102,7 @@ struct WindowArgs {
     int32_t window, sinks;
     int32_t total_tokens, max_new_tokens, force_rows;   // as in PrefillArgs
     int32_t parts, items;        // workgroups that share a range or tile; tiles of a head (filled in by the launcher)
+    uint64_t tag;                // as in PrefillArgs
 };
 hipError_t launch_decode_window(const WindowArgs &a, hipStream_t stream);
 hipError_t launch_prefill_window(const WindowArgs &a, hipStream_t stream);

@@ -936,6 +936,7 @@ int lamps_prefill_attn_window(lamps_ctx *c, int32_t layer, int32_t n_req, int32_
         w.total_tokens = total_tokens;
         w.max_new_tokens = max_new_tokens > 0 && max_new_tokens < total_tokens ? max_new_tokens : total_tokens;
         w.force_rows = max_new_tokens < 0;
+        w.tag = lamps::next_launch_tag();
         LAMPS_HIP(lamps::launch_prefill_window(w, c->cs));
         return LAMPS_OK;
     }

@@ -11,6 +11,7 @@
 #include <type_traits>
 
 #include "attn_reducers.h"
+#include "handover.h"
 #include "internal.h"
 #include "requests.h"
 #include "tile_parts.h"
@@ -467,12 +468,12 @@ hipError_t launch_tiles(WindowArgs w, hipStream_t s)
     const long long items = (long long)w.total_tokens / WT + a.batch, tiles = items * a.num_kv_heads;
     const long long stages = (std::min((long long)a.max_blocks * a.block_size, (long long)w.window + w.sinks + WT) + 31) / 32 + 1;
     const long long state = (long long)tile_state_floats(D, kWaves * 16 * kCB) * (long long)sizeof(float);
-    // Two workgroups fit a CU, 512 the chip: with twice as many parts 12 responses of 4 to 64 tokens, window 2 048, took 49 us, 45 so, and one prompt of 2 000 (504
-    // tiles) 53 us, 31 whole.  Four stages at least to a part: a part's way to its first product is as long as four.
+    // Two workgroups fit a CU, 512 the chip: with half as many parts more 12 responses of 4 to 64 tokens, window 2 048, took 46 us, 40 so, and one prompt of 2 000 (504
+    // tiles) in two 55 us, 31 whole.  Four stages at least to a part: a part's way to its first product is as long as four.
     // (about as many tiles as there are: half of the requests' last ones are there besides the full ones)
     const long long there = std::max(1LL, ((long long)w.total_tokens / WT + a.batch / 2) * a.num_kv_heads);
     long long parts = std::min(512 / there, stages / 4);
-    parts = std::max(1LL, std::min({parts, (long long)kMostParts, (long long)a.partial_capacity / (state * tiles)}));
+    parts = std::max(1LL, std::min({parts, (long long)kMostParts, (long long)a.partial_capacity / ((state + 8) * tiles)}));
     const long long grid = (tiles * parts + 7) / 8 * 8, join = (tiles + 7) / 8 * 8;
     if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
     w.items = (int)items;
@@ -483,11 +484,8 @@ hipError_t launch_tiles(WindowArgs w, hipStream_t s)
     }
     hipLaunchKernelGGL((window_tiles<D, TILED, kCB, true>), dim3((unsigned)grid), dim3(kThreads), 0, s, w);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if (parts <= 4)
-        hipLaunchKernelGGL((window_join<D, kCB, true>), dim3((unsigned)join, kWaves * kCB, (D + 127) / 128), dim3(kThreads), 0, s, w);
-    else
-        hipLaunchKernelGGL((window_join<D, kCB, false>), dim3((unsigned)join, kWaves * kCB, D / 32), dim3(kThreads), 0, s, w);
+    if (e != hipSuccess || parts <= kHandedParts) return e;
+    hipLaunchKernelGGL((window_join<D, kCB>), dim3((unsigned)join, kWaves * kCB, D / 32), dim3(kThreads), 0, s, w);
     return hipGetLastError();
 }
 

@@ -9,8 +9,9 @@
 // with zeros, multiply once per token of the wave, with what that one does not see zeroed.
 //
 // Bound by the matrix cores and the vector ALUs on long prompts, as prefill_mfma is, and by the walk where few tokens leave the chip idle: then
-// the stages of a tile are shared by `parts` workgroups, as many as the host counts from window and sinks, and a second launch adds them up
-// (12 responses of 4 to 64 tokens on 32 / 8 heads, window 2 048: 36 us and 7).
+// the stages of a tile are shared by up to `parts` workgroups, as many as the host counts from window and sinks.  Up to four parts are added up by the last of them to
+// arrive, more by a second launch (us, so / by a second launch always: 12 responses of 4 to 64 tokens on 32 / 8 heads, window 2 048, in two 40.3 / 43.5;
+// 12 of 6 to 35 on 345 to 2 490, window of everything, 30.3 / 33.4; 4 of 16, 40 plain heads, 40.3 / 44.8; one of 16 tokens on 32 / 8, in 16, 18.6 / 13.8).
 
 // Which workgroup does what: items -- tiles of one head, numbered by the row that they begin at, at most one for nothing per request -- head by
 // head, and of these an eighth, one after the other, to each of the eight XCDs: neighbours in time and place share most of their windows in an L2.
@@ -49,9 +50,10 @@ __device__ __forceinline__ bool tile_at(const WindowArgs &w, int WT, TileAt &at,
 constexpr size_t tile_state_floats(int D, int columns) { return (size_t)columns * (D + 2); }
 
 // Narrow tiles, of 64 columns, whole: one stage per barrier, operands read one after the other, for three or four workgroups to a CU.  Shared ones
-// keep four stages in LDS instead (12 responses 43.6 us, 45.2 as whole ones have it).
+// keep four stages in LDS instead (12 responses, added up by a second launch, 43.6 us, 45.2 as whole ones have it).
 template <int D, int kCB, bool SPLIT>
 constexpr bool tile_small() { return D <= 128 && kCB == 1 && !SPLIT; }
+constexpr int kHandedParts = 4;
 // Stages per barrier, and groups of them that LDS holds.
 template <int D, int kCB>
 constexpr int tile_groups() { return D <= 128 && kCB > 1 ? 2 : 1; }
@@ -83,9 +85,15 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : (tile_small<D, 
     const int p_first = base_pos + at.tile * WT, p_last = base_pos + min(n_new, (at.tile + 1) * WT) - 1;
     const Sight<16> see(p_last + 1, max(0, p_first - w.window + 1), w.sinks, std::true_type{});
     const int last_unit = see.units - 1, n_stages = (see.units + 1) / 2;
-    int st0 = 0, st1 = n_stages;
+    int st0 = 0, st1 = n_stages, runs = 1;
     if constexpr (SPLIT) {
-        const int each = (((n_stages + w.parts - 1) / w.parts) + GRP - 1) / GRP * GRP;
+        // (parts are whole groups; handed over in here, eight stages at least, or twelve, whose states are twice as large: 4 of 64 tokens, 16 plain heads of 256, 35.8 us by
+        // eight, 30.6 so; of 128 all the same)
+        const bool handed = w.parts <= kHandedParts;
+        runs = handed ? max(1, min(w.parts, n_stages / (D >= 256 ? 12 : 8))) : w.parts;
+        const int each = ((n_stages + runs - 1) / runs + GRP - 1) / GRP * GRP;
+        if (handed) runs = (n_stages + each - 1) / each;
+        if (at.part >= runs) return;
         st0 = min(n_stages, at.part * each);
         st1 = min(n_stages, st0 + each);
     }
@@ -383,7 +391,7 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : (tile_small<D, 
     }
     __builtin_amdgcn_s_waitcnt(vmcnt(0));             // no load is left on its way to LDS
 
-    if constexpr (SPLIT) {
+    if (SPLIT && w.parts > kHandedParts) {
         // the columns of each block as the wave holds them, by whole lines, and their (reference, sum)
         if (none) return;
         float *mine = a.partials + ((size_t)at.item * w.parts + at.part) * tile_state_floats(D, kWaves * kCols);
@@ -394,16 +402,86 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : (tile_small<D, 
             for (int s = 0; s < NS; ++s) *reinterpret_cast<f32x4 *>(to + s * 256 + 4 * lane) = o[b][s];
             if (qd == 0) *reinterpret_cast<float2 *>(mine + (size_t)kWaves * kCols * D + 2 * ((wv * kCB + b) * 16 + j)) = make_float2(m[b], l[b][0]);
         }
-    } else {
-#pragma unroll
-        for (int b = 0; b < kCB; ++b) store_column<NS>(static_cast<uint16_t *>(a.out) + orow[b], qd, pos[b] >= 0, 1.0f / l[b][0], o[b]);
+        return;
     }
+    if (SPLIT && runs > 1) {
+        // the columns of each block as the wave holds them, and their (reference, sum); the last part to arrive adds them up
+        constexpr int kAll = kWaves * kCols;
+        const size_t state = tile_state_floats(D, kAll);
+        float *first_part = a.partials + (size_t)at.item * w.parts * state, *to = first_part + at.part * state;
+        uint64_t *flags = reinterpret_cast<uint64_t *>(a.partials + (size_t)w.items * a.num_kv_heads * w.parts * state) + (size_t)at.item * w.parts;
+        if (!none) {
+#pragma unroll
+            for (int b = 0; b < kCB; ++b) {
+                const int block = wv * kCB + b;
+#pragma unroll
+                for (int s = 0; s < 2 * NS; ++s)
+                    put_shared(to + block * 16 * D + s * 128 + 2 * lane, o[b][s >> 1][2 * (s & 1)], o[b][s >> 1][2 * (s & 1) + 1]);
+                if (qd == 0) put_shared(to + kAll * D + 2 * (block * 16 + j), m[b], l[b][0]);
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(vmcnt(0));
+        __syncthreads();                              // the workgroup's stores have arrived, and its LDS is free
+        int *is_last = reinterpret_cast<int *>(lds);
+        if (wv == 0) {
+            const bool all = report_run<false>(flags, 1, at.part, runs, w.tag);
+            if (lane == 0) *is_last = all;
+        }
+        __syncthreads();
+        if (!*is_last) return;
+        // The parts in order, whichever workgroup this is: bit-reproducible.  The waves share the blocks that have columns, by halves of their dims.
+        constexpr int HS = NS / 2, N = kHandedParts;
+        int me = lane;
+        asm volatile("" : "+v"(me));                  // (worked out here, not kept over the loop)
+        const int j = me & 15, qd = me >> 4;
+        const int blocks = (min(WT, n_new - at.tile * WT) + TW - 1) / TW * kCB;
+#pragma unroll 1
+        for (int u = wv; u < 2 * blocks; u += kWaves) {
+            const int block = u >> 1, half = u & 1;
+            float2 ml[N], x[N][2 * HS];
+            float M = kLeast, L = 0.0f;
+            f32x4 A[HS];
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                if (k > 1 && k >= runs) {             // uniform
+                    ml[k] = make_float2(kLeast, 0.0f);
+#pragma unroll
+                    for (int s = 0; s < 2 * HS; ++s) x[k][s] = make_float2(0.0f, 0.0f);
+                    continue;
+                }
+                const float *from = first_part + k * state;
+                ml[k] = get_shared(from + kAll * D + 2 * (block * 16 + j));
+#pragma unroll
+                for (int s = 0; s < 2 * HS; ++s) x[k][s] = get_shared(from + block * 16 * D + (half * 2 * HS + s) * 128 + 2 * me);
+            }
+#pragma unroll
+            for (int k = 0; k < N; ++k) M = fmaxf(M, ml[k].x);
+#pragma unroll
+            for (int s = 0; s < HS; ++s) A[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const float f = fast_exp2(ml[k].x - M);
+                L += ml[k].y * f;
+#pragma unroll
+                for (int s = 0; s < 2 * HS; ++s) {
+                    A[s >> 1][2 * (s & 1)] += x[k][s].x * f;
+                    A[s >> 1][2 * (s & 1) + 1] += x[k][s].y * f;
+                }
+            }
+            const int c = block % kCB * 16 + j, t = c / G, tok = at.tile * WT + block / kCB * TW + t;
+            const bool mine = c < TW * G && tok < n_new;
+            store_column<HS>(static_cast<uint16_t *>(a.out) + ((size_t)(first + (mine ? tok : 0)) * a.num_q_heads + g * G + (mine ? c - t * G : 0)) * D + 16 * half * HS, qd,
+                             mine, 1.0f / L, A);
+        }
+        return;
+    }
+#pragma unroll
+    for (int b = 0; b < kCB; ++b) store_column<NS>(static_cast<uint16_t *>(a.out) + orow[b], qd, pos[b] >= 0, 1.0f / l[b][0], o[b]);
 }
 
-// Adds the parts of a tile up, two slabs of 16 columns at a time: a wave alone where there are up to four parts, else the four waves of a workgroup every
-// fourth part each (16 parts of 8 tiles 7.0 us alone, 4.0 together; 2 parts of 300 tiles 7.8 and 13).  What they add is asked for in front of the
-// lengths that say which rows it is (where it lies goes by the launch alone).
-template <int D, int kCB, bool ALONE>
+// Adds more than kHandedParts parts of a tile up, two slabs of 16 columns to a workgroup, every fourth part to a wave.  What they add is asked for in front of
+// the lengths that say which rows it is (where it lies goes by the launch alone).
+template <int D, int kCB>
 __global__ __launch_bounds__(kThreads) void window_join(const WindowArgs w0)
 {
     constexpr int kCols = 16 * kCB, N = 4, MOST = kMostParts / kWaves;
@@ -414,9 +492,7 @@ __global__ __launch_bounds__(kThreads) void window_join(const WindowArgs w0)
     w.parts = 1;
     const int G = a.num_q_heads / a.num_kv_heads, TW = kCols / G, WT = kWaves * TW, parts = w0.parts;
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 15, qd = lane >> 4;
-    constexpr int STEP = ALONE ? 1 : kWaves;
-    const int block = blockIdx.y, slab = 2 * (ALONE ? blockIdx.z * kWaves + wv : blockIdx.z), from0 = ALONE ? 0 : wv;
-    if (slab >= D / 16) return;
+    const int block = blockIdx.y, slab = 2 * blockIdx.z;
     const size_t state = tile_state_floats(D, kWaves * kCols);
     const int item = tile_item(w, blockIdx.x, a.num_kv_heads);
     if (item < 0) return;
@@ -440,7 +516,7 @@ __global__ __launch_bounds__(kThreads) void window_join(const WindowArgs w0)
         f32x4 y[N][2];
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const float *from = x + (size_t)min(from0 + STEP * (k0 + k), parts - 1) * state;
+            const float *from = x + (size_t)min(wv + kWaves * (k0 + k), parts - 1) * state;
             ml[k] = *reinterpret_cast<const float2 *>(from + (size_t)kWaves * kCols * D + 2 * (block * 16 + j));
 #pragma unroll
             for (int s = 0; s < 2; ++s) y[k][s] = *reinterpret_cast<const f32x4 *>(from + (size_t)block * 16 * D + (slab + s) * 256 + 4 * lane);
@@ -451,20 +527,18 @@ __global__ __launch_bounds__(kThreads) void window_join(const WindowArgs w0)
         }
 #pragma unroll
         for (int k = 0; k < N; ++k)
-            if (from0 + STEP * (k0 + k) < parts) add(ml[k], y[k][0], y[k][1]);
-        if (STEP * (k0 + N) >= parts) break;
+            if (wv + kWaves * (k0 + k) < parts) add(ml[k], y[k][0], y[k][1]);
+        if (kWaves * (k0 + N) >= parts) break;
     }
-    if constexpr (!ALONE) {
-        sums[wv][0][lane] = make_float4(A[0][0], A[0][1], A[0][2], A[0][3]);
-        sums[wv][1][lane] = make_float4(A[1][0], A[1][1], A[1][2], A[1][3]);
-        stats[wv][lane] = make_float2(M, L);
-        __syncthreads();
-        if (wv > 0) return;
+    sums[wv][0][lane] = make_float4(A[0][0], A[0][1], A[0][2], A[0][3]);
+    sums[wv][1][lane] = make_float4(A[1][0], A[1][1], A[1][2], A[1][3]);
+    stats[wv][lane] = make_float2(M, L);
+    __syncthreads();
+    if (wv > 0) return;
 #pragma unroll
-        for (int k = 1; k < kWaves; ++k) {
-            const float4 y0 = sums[k][0][lane], y1 = sums[k][1][lane];
-            add(stats[k][lane], f32x4{y0.x, y0.y, y0.z, y0.w}, f32x4{y1.x, y1.y, y1.z, y1.w});
-        }
+    for (int k = 1; k < kWaves; ++k) {
+        const float4 y0 = sums[k][0][lane], y1 = sums[k][1][lane];
+        add(stats[k][lane], f32x4{y0.x, y0.y, y0.z, y0.w}, f32x4{y1.x, y1.y, y1.z, y1.w});
     }
     const int n_new = min(at.n_new, w.total_tokens - at.first);
     const int wave_tok = at.tile * WT + block / kCB * TW, c = block % kCB * 16 + j, tl = c / G;

@@ -313,3 +313,57 @@ def test_prefill_heads_of_256_in_groups(dtype, H, Hkv, D, bs, reqs, looks):
 @pytest.mark.parametrize("reqs,window,at", [([(300, 300), (200, 20)], 40, (100, 185)), ([(900, 20), (700, 9)], 600, (895, 100))])
 def test_values_and_keys_that_are_no_numbers_heads_of_256(reqs, window, at):
     test_values_and_keys_that_are_no_numbers_in_large_and_shared_launches("bf16", 8, 4, 256, reqs, window, at)
+
+
+#          few tiles with long walks, in two to four parts that the last workgroup of a tile adds up
+SHARED = [
+    ("bf16", 32, 8, 128, 16, [(1500, 40), (900, 37), (30, 30), (1200, 64), (800, 1), (1100, 40)], [(1000, 4), (2000, 0)]),
+    ("bf16", 32, 8, 128, 32, [(1500, 150), (900, 141), (300, 300)], [(1000, 4)]),
+    ("bf16", 8, 8, 128, 16, [(1300, 300), (900, 290), (1700, 310)], [(700, 33)]),
+    ("bf16", 16, 8, 64, 16, [(1500, 150), (1100, 140), (900, 170)], [(800, 3)]),
+    ("bf16", 16, 8, 256, 16, [(3500, 832)], [(3000, 5)]),
+    ("bf16", 8, 8, 256, 16, [(1500, 460), (1200, 440)], [(600, 2)]),
+]
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,D,bs,reqs,looks", SHARED)
+def test_prefill_of_shared_tiles(dtype, H, Hkv, D, bs, reqs, looks):
+    test_prefill(dtype, H, Hkv, D, bs, reqs, looks, False)
+
+
+def test_values_and_keys_that_are_no_numbers_in_shared_tiles():
+    test_values_and_keys_that_are_no_numbers_in_large_and_shared_launches(
+        "bf16", 32, 8, 128, [(1500, 40), (900, 37), (30, 30), (1200, 64), (800, 9), (1100, 40)], 1000, (490, 890, 3, 180, 795, 1070))
+
+
+def test_shared_tiles_replayed():
+    """A captured call whose tiles are shared, replayed with other calls of the same workspace in between."""
+    reqs, window, sinks = [(1500, 40), (900, 37), (30, 30), (1200, 64), (800, 1), (1100, 40)], 1000, 4
+    geom, rig, table, K, V, ctx = _setup("bf16", 32, 8, 128, 16, reqs, window, sinks, 12)
+    dev, total, lam = rig.dev, sum(n for _, n in reqs), rig.lamps
+    start = torch.tensor(np.concatenate([[0], np.cumsum([n for _, n in reqs])]), dtype=torch.int32, device=dev)
+    td, cd = torch.as_tensor(table, device=dev), torch.tensor(ctx, dtype=torch.int32, device=dev)
+    queries = [n2t(W.queries(s, geom, total), dev) for s in range(3)]
+    with torch.cuda.stream(rig.compute):
+        want = [torch.zeros_like(q) for q in queries]
+        for q, out in zip(queries, want):
+            lam.prefill_attn_window(1, 6, total, window, sinks, q, start, td, cd, out, max_new_tokens=64)
+        q, out, other, ones = queries[0].clone(), torch.zeros_like(queries[0]), torch.zeros_like(queries[0]), torch.ones(6, dtype=torch.uint8, device=dev)
+        rig.compute.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=rig.compute):
+            lam.prefill_attn_window(1, 6, total, window, sinks, q, start, td, cd, out, max_new_tokens=64)
+            lam.prefill_attn_window(1, 6, total, window, sinks, out, start, td, cd, other, max_new_tokens=64)
+        for it in range(6):
+            q.copy_(queries[it % 3])
+            out.zero_()
+            graph.replay()
+            again = torch.zeros_like(q)
+            lam.prefill_attn_window(1, 6, total, window, sinks, out, start, td, cd, again, max_new_tokens=64)
+            rig.compute.synchronize()
+            assert torch.equal(out, want[it % 3]) and torch.equal(other, again), it
+            lam.decode_attn_window(1, 6, 900, 0, q[:6], td, cd, ones, torch.zeros_like(q[:6]))
+            if it % 2:
+                lam.prefill_attn_window(1, 6, total, 300, 0, q, start, td, cd, torch.zeros_like(q), max_new_tokens=64)
+    torch.cuda.synchronize()
+    rig.close()
