@@ -124,6 +124,9 @@ class LiveEngine:
     def _batch(self, rids, cached, counts):
         """The batch's table, lengths before and after its new tokens, and first rows, made on the device."""
         bs, row, n = self.cfg.block_size, self.cfg.max_blocks_per_req, len(rids)
+        for r, c, k in zip(rids, cached, counts):   # (batch_tables would leave it out of the batch)
+            if c + k > row * bs:
+                raise ValueError("request %d has %d positions, a row of the block table holds %d" % (r, c + k, row * bs))
         ids = [b for r, c, k in zip(rids, cached, counts) for b in self.blocks[r][:(c + k + bs - 1) // bs]]
         given = torch.tensor(list(cached) + list(counts) + ids, dtype=torch.int32).to(self.dev)
         made = torch.empty(n * (row + 2) + 1, dtype=torch.int32, device=self.dev)
