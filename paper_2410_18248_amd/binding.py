@@ -40,7 +40,8 @@ class LampsConfig(ctypes.Structure):
 
 
 class LampsRope(ctypes.Structure):
-    """``lamps_rope``.  `frequencies`, `q_weight` and `k_weight` are device memory, which this object keeps alive where it is a tensor."""
+    """``lamps_rope``.  `frequencies`, `q_weight` and `k_weight` are device memory, which this object keeps alive where it is a tensor; a call
+    refuses tensors in host memory, and weights that are not head_dim numbers of its cache's type."""
     _fields_ = [("rotary_dim", ctypes.c_int32), ("pairs", ctypes.c_int32), ("normalise", ctypes.c_int32),
                 ("norm_eps", ctypes.c_float), ("amplitude", ctypes.c_float), ("frequencies", ctypes.c_void_p),
                 ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p)]
@@ -56,7 +57,18 @@ class LampsRope(ctypes.Structure):
         super().__init__(rotary_dim, pairs, 1 if normalise else 0, norm_eps, amplitude, _ptr(frequencies) or None,
                          _ptr(q_weight) or None, _ptr(k_weight) or None)
         self._keep = (frequencies, q_weight, k_weight)
+        self._suits = None                              # the last form that it was found to suit
         self.address = ctypes.addressof(self)
+
+    def suit(self, form):
+        """Raises if a tensor of this rope is not what a cache of form = (dtype, head_dim) reads."""
+        for name, x in zip(("frequencies", "q_weight", "k_weight"), self._keep):
+            if hasattr(x, "is_cuda") and not x.is_cuda or hasattr(x, "__array_interface__"):
+                raise LampsError(-1, "LampsRope: %s is in host memory" % name)
+            if name != "frequencies" and hasattr(x, "element_size"):
+                if str(x.dtype) != ("torch.bfloat16" if form[0] == LAMPS_BF16 else "torch.float32") or x.numel() != form[1]:
+                    raise LampsError(-1, "LampsRope: %s must be head_dim (%d) numbers of the cache's type" % (name, form[1]))
+        self._suits = form
 
 
 def lib_path():
@@ -282,6 +294,17 @@ def _ptr(x):
     return ctypes.cast(x, ctypes.c_void_p).value
 
 
+def _rows(x, stride, name):
+    """The address of rows that are `stride` elements apart, 0: that follow each other."""
+    try:
+        if stride or x.is_contiguous():
+            return x.data_ptr()
+    except AttributeError:              # (no tensor)
+        return _ptr(x)
+    raise LampsError(-1, "%s: its rows do not follow each other; its stride is wanted" % name if stride is not None else
+                     "%s must be contiguous" % name)
+
+
 def _ids(block_ids):
     ids = list(block_ids)
     return (ctypes.c_int32 * max(len(ids), 1))(*ids), len(ids)
@@ -336,6 +359,7 @@ class Lamps:
                  swap_in_stream=0):
         self.lib = load_library()
         self.cfg = cfg
+        self._form = (cfg.dtype, cfg.head_dim)
         self._keep = (k_pool, v_pool, workspace)     # the caller's memory must outlive the context
         h = ctypes.c_void_p()
         rc = self.lib.lamps_create(ctypes.byref(cfg), _ptr(k_pool), _ptr(v_pool), _ptr(workspace),
@@ -398,16 +422,22 @@ class Lamps:
 
     def rope_append(self, layer, batch, rope, q, k_new, v_new, block_table, ctx_lens, running_mask, advance, q_out,
                     q_stride=0, k_stride=0, v_stride=0):
-        """Strides in elements; 0: rows follow each other (they are not taken from a tensor's own strides)."""
-        self._check(self.lib.lamps_rope_append(self.h, layer, batch, rope.address, _ptr(q), q_stride, _ptr(k_new), k_stride, _ptr(v_new),
-                                               v_stride, _ptr(block_table), _ptr(ctx_lens), _ptr(running_mask),
-                                               1 if advance else 0, _ptr(q_out)))
+        """Strides in elements; 0: rows follow each other (tensors whose rows do not are refused)."""
+        if rope._suits is not self._form:
+            rope.suit(self._form)
+        self._check(self.lib.lamps_rope_append(self.h, layer, batch, rope.address, _rows(q, q_stride, "q"), q_stride,
+                                               _rows(k_new, k_stride, "k_new"), k_stride, _rows(v_new, v_stride, "v_new"), v_stride,
+                                               _ptr(block_table), _ptr(ctx_lens), _ptr(running_mask), 1 if advance else 0,
+                                               _rows(q_out, None, "q_out")))
 
     def rope_append_tokens(self, layer, n_req, total_tokens, rope, q, k_new, v_new, q_start, block_table, ctx_lens, q_out,
                            q_stride=0, k_stride=0, v_stride=0):
-        self._check(self.lib.lamps_rope_append_tokens(self.h, layer, n_req, total_tokens, rope.address, _ptr(q), q_stride, _ptr(k_new),
-                                                      k_stride, _ptr(v_new), v_stride, _ptr(q_start), _ptr(block_table),
-                                                      _ptr(ctx_lens), _ptr(q_out)))
+        if rope._suits is not self._form:
+            rope.suit(self._form)
+        self._check(self.lib.lamps_rope_append_tokens(self.h, layer, n_req, total_tokens, rope.address, _rows(q, q_stride, "q"), q_stride,
+                                                      _rows(k_new, k_stride, "k_new"), k_stride, _rows(v_new, v_stride, "v_new"),
+                                                      v_stride, _ptr(q_start), _ptr(block_table), _ptr(ctx_lens),
+                                                      _rows(q_out, None, "q_out")))
 
     def batch_tables(self, n_req, total_tokens, cached, new_tokens, block_ids, n_ids, grow, block_table, ctx_lens, q_start,
                      slots=None, report=None):
