@@ -106,7 +106,7 @@
     const bf16x8 ones = __builtin_bit_cast(bf16x8, ones_u);
 #pragma unroll
     for (int b = 0; b < kCB; ++b) {
-        m[b] = kLowest;
+        m[b] = WINDOW ? kLeast : kLowest;            // (as window_tiles, as prefill_mfma)
         l[b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < NS; ++s) o[b][s] = f32x4{0.f, 0.f, 0.f, 0.f};

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <cfloat>
 #include <type_traits>
 
 namespace lamps {
@@ -10,6 +11,7 @@ namespace {
 
 constexpr int kStage = 32;               // cached positions per LDS stage
 constexpr float kSlack = 8.0f;           // log2 of the largest weight before the reference moves
+constexpr float kLeast = -FLT_MAX;       // a reference below which no finite score lies
 
 typedef __attribute__((address_space(4))) const int32_t *table_ptr;   // read-only: scalar loads
 

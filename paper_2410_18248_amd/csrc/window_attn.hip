@@ -7,7 +7,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cfloat>
 #include <type_traits>
 
 #include "attn_reducers.h"
@@ -20,8 +19,6 @@ namespace lamps {
 namespace {
 
 // ---------------------------------------------------------------- what a token sees
-
-constexpr float kLeast = -FLT_MAX;       // a reference below which no finite score lies
 
 // A state without a position is (kLeast, 0, 0).  A row of no positions is zero; one whose weights are not numbers is none either.
 __device__ __forceinline__ float reciprocal(float L, bool none) { return none ? 0.0f : 1.0f / L; }
