@@ -438,6 +438,7 @@
     }
     __builtin_amdgcn_s_waitcnt(vmcnt(0));            // no load of the wave's is left on its way to LDS
     if (!team) barrier();
+    if constexpr (WINDOW) products_there(l, o);
 #pragma unroll
     for (int b = 0; b < kCB; ++b) {
         const float lt = l[b][0];
