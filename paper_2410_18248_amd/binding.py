@@ -57,17 +57,20 @@ class LampsRope(ctypes.Structure):
         super().__init__(rotary_dim, pairs, 1 if normalise else 0, norm_eps, amplitude, _ptr(frequencies) or None,
                          _ptr(q_weight) or None, _ptr(k_weight) or None)
         self._keep = (frequencies, q_weight, k_weight)
+        named = tuple(zip(("frequencies", "q_weight", "k_weight"), self._keep))
+        self._host = [n for n, x in named if not getattr(x, "is_cuda", True) or hasattr(x, "__array_interface__")]
+        types = {"torch.bfloat16": LAMPS_BF16, "torch.float32": LAMPS_F32}
+        self._weights = [(n, (types.get(str(x.dtype)), x.numel())) for n, x in named[1:] if hasattr(x, "element_size")]
         self._suits = None                              # the last form that it was found to suit
         self.address = ctypes.addressof(self)
 
     def suit(self, form):
         """Raises if a tensor of this rope is not what a cache of form = (dtype, head_dim) reads."""
-        for name, x in zip(("frequencies", "q_weight", "k_weight"), self._keep):
-            if hasattr(x, "is_cuda") and not x.is_cuda or hasattr(x, "__array_interface__"):
-                raise LampsError(-1, "LampsRope: %s is in host memory" % name)
-            if name != "frequencies" and hasattr(x, "element_size"):
-                if str(x.dtype) != ("torch.bfloat16" if form[0] == LAMPS_BF16 else "torch.float32") or x.numel() != form[1]:
-                    raise LampsError(-1, "LampsRope: %s must be head_dim (%d) numbers of the cache's type" % (name, form[1]))
+        if self._host:
+            raise LampsError(-1, "LampsRope: %s is in host memory" % self._host[0])
+        for name, has in self._weights:
+            if has != form:
+                raise LampsError(-1, "LampsRope: %s must be head_dim (%d) numbers of the cache's type" % (name, form[1]))
         self._suits = form
 
 
@@ -294,15 +297,14 @@ def _ptr(x):
     return ctypes.cast(x, ctypes.c_void_p).value
 
 
-def _rows(x, stride, name):
-    """The address of rows that are `stride` elements apart, 0: that follow each other."""
+def _rows(x):
+    """The address of rows that follow each other."""
     try:
-        if stride or x.is_contiguous():
+        if x.is_contiguous():
             return x.data_ptr()
     except AttributeError:              # (no tensor)
         return _ptr(x)
-    raise LampsError(-1, "%s: its rows do not follow each other; its stride is wanted" % name if stride is not None else
-                     "%s must be contiguous" % name)
+    raise LampsError(-1, "q_out must be contiguous, and so must q, k_new and v_new where no stride is given")
 
 
 def _ids(block_ids):
@@ -425,19 +427,19 @@ class Lamps:
         """Strides in elements; 0: rows follow each other (tensors whose rows do not are refused)."""
         if rope._suits is not self._form:
             rope.suit(self._form)
-        self._check(self.lib.lamps_rope_append(self.h, layer, batch, rope.address, _rows(q, q_stride, "q"), q_stride,
-                                               _rows(k_new, k_stride, "k_new"), k_stride, _rows(v_new, v_stride, "v_new"), v_stride,
+        self._check(self.lib.lamps_rope_append(self.h, layer, batch, rope.address, (_ptr if q_stride else _rows)(q), q_stride,
+                                               (_ptr if k_stride else _rows)(k_new), k_stride, (_ptr if v_stride else _rows)(v_new), v_stride,
                                                _ptr(block_table), _ptr(ctx_lens), _ptr(running_mask), 1 if advance else 0,
-                                               _rows(q_out, None, "q_out")))
+                                               _rows(q_out)))
 
     def rope_append_tokens(self, layer, n_req, total_tokens, rope, q, k_new, v_new, q_start, block_table, ctx_lens, q_out,
                            q_stride=0, k_stride=0, v_stride=0):
         if rope._suits is not self._form:
             rope.suit(self._form)
-        self._check(self.lib.lamps_rope_append_tokens(self.h, layer, n_req, total_tokens, rope.address, _rows(q, q_stride, "q"), q_stride,
-                                                      _rows(k_new, k_stride, "k_new"), k_stride, _rows(v_new, v_stride, "v_new"),
+        self._check(self.lib.lamps_rope_append_tokens(self.h, layer, n_req, total_tokens, rope.address, (_ptr if q_stride else _rows)(q), q_stride,
+                                                      (_ptr if k_stride else _rows)(k_new), k_stride, (_ptr if v_stride else _rows)(v_new),
                                                       v_stride, _ptr(q_start), _ptr(block_table), _ptr(ctx_lens),
-                                                      _rows(q_out, None, "q_out")))
+                                                      _rows(q_out)))
 
     def batch_tables(self, n_req, total_tokens, cached, new_tokens, block_ids, n_ids, grow, block_table, ctx_lens, q_start,
                      slots=None, report=None):
