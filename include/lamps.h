@@ -353,8 +353,12 @@ int lamps_decode_attn_window(lamps_ctx *ctx, int32_t layer, int32_t batch, int32
  * t <= p with t > p - window or t < sinks.  What counts for none of a request's new
  * tokens is not read, nor are the table entries of blocks that hold nothing else;
  * what does not count for one of them has no part in its row.  Rows, arguments,
- * max_new_tokens, types, order and workspace are as for lamps_prefill_attn (bf16:
- * weights rounded to bf16 before the second product, except by a wavefront per token).
+ * max_new_tokens, types, order and workspace are as for lamps_prefill_attn, but that a
+ * max_new_tokens that is too small leaves no row unwritten.  bf16: weights are rounded
+ * to bf16 before the second product and summed as rounded (rows of normal values are off by
+ * 0.0023 of their size, 0.0017 of it by their own rounding), except by a wavefront per
+ * token, max_new_tokens < 0; and scores beyond 2^30 in size, which 32 bits hold to no
+ * better than 64, may make a row NaN.
  * Errors: INVALID (null, alignment, window < 1, sinks < 0), RANGE (layer, n_req >
  * max_batch, negative sizes). */
 int lamps_prefill_attn_window(lamps_ctx *ctx, int32_t layer, int32_t n_req, int32_t total_tokens,

@@ -9,7 +9,8 @@
 // Bound by the launch and the round trips: lengths, the sums, ids (and kept entries), stores.  One launch: every workgroup sums the
 // whole batch up for itself, which is a load per request of a thread and two scans, keeps what its own part asks for in LDS, and writes that part:
 // 2 048 entries of the table, a request's whole row at most, or 1 024 slots; the first one writes lengths and first rows.  A second launch behind one that sums
-// costs more than the sums do.  64 requests with rows of 512: 4.8 us; 1 024 with rows of 2 048, 8 MB of table, and 206 000 slots: 9.9.
+// costs more than the sums do, up to 1 024 requests: 64 with rows of 512 4.8 us; 1 024 with rows of 2 048, 8 MB of table, and 206 000 slots, 9.5.  Beyond, a thread sums up to 32 requests
+// and every part does so again: 1 025 with rows of 512 / 2 048 take 23 / 56 us (1 024: 5.6 / 7.9), 8 192 180 / 660, of which the stores are 3 / 13.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

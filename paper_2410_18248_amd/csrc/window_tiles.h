@@ -8,6 +8,10 @@
 // not reach the columns that do not see it (a zero weight does not silence it): stages that hold one, which is found by a product of the values
 // with zeros, multiply once per token of the wave, with what that one does not see zeroed.
 //
+// Weights are rounded to bf16 for the second product and summed up as rounded, in fp32: outputs of normal values are off by 0.0021 to 0.0023 of their size, 0.0016 to
+// 0.0017 of that by their own rounding.  As pairs of bf16, which decode has, they are off by that alone, and launches take 1.03 to 1.33 times as long
+// (4 x 8 192 tokens, window 1 024, 588 / 743 us; 12 responses 37.6 / 43.5); a wavefront per token, which a caller can ask for, has them in fp32.
+//
 // Bound by the matrix cores and the vector ALUs on long prompts, as prefill_mfma is, and by the walk where few tokens leave the chip idle: then
 // the stages of a tile are shared by up to `parts` workgroups, as many as the host counts from window and sinks.  Up to four parts are added up by the last of them to
 // arrive, more by a second launch (us, so / by a second launch always: 12 responses of 4 to 64 tokens on 32 / 8 heads, window 2 048, in two 40.3 / 43.5;
@@ -567,7 +571,7 @@ __global__ __launch_bounds__(kThreads) void window_join(const WindowArgs w0)
 // prefill_teams' way through a tile of 256 columns (128 at head size 256), for launches with many new tokens (grouped heads: plain ones are as fast or faster by
 // window_tiles).
 // Bound by the two teams' phases in turn, matrix cores and vector ALUs; what a tile costs beyond its stages, its queries and outputs, two masked ends and the filling of
-// the pipeline, is 11 of 35 us under a window of 1 024: 4 prompts of 8 192 on 32 / 8 heads take 565 us, 915 TFLOP/s of the positions seen.  Tiles in
+// the pipeline, is 11 of 35 us under a window of 1 024: 4 prompts of 8 192 on 32 / 8 heads take 555 to 600 us from card to card, 860 to 930 TFLOP/s of the positions seen.  Tiles in
 // chains, the next one's first stages asked for behind the last one's, took 580 to 600.
 template <int D, int kCB>
 __global__ __launch_bounds__(512, 2) void window_teams(const WindowArgs w)

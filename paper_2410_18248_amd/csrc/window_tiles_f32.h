@@ -5,7 +5,9 @@
 // operands and sums (MfmaF32Tile) these are; its four waves take every fourth of the units that the tile's tokens see and add their states up in LDS.
 // Units that some column does not see whole are masked, and values there that are no finite numbers kept from the columns that do not see them.
 // In large launches with short walks a wave has a tile of its own.
-// Bound by the walk on short prompts (6 of 17 to 700 tokens, 8 heads of 64, window 100: 17 us, of which the matrix rate is 4), by the fp32 matrix rate on long ones.
+// Bound by the walk on short prompts (6 of 17 to 700 tokens, 8 heads of 64, window 100: 16 us, 4 of them bytes), by keys and values out of L2 on long ones: a wave
+// loads a unit's for its own 16 columns alone, 8 flops a byte at head size 128.  4 of 700 tokens on 500, 32 / 8 heads, 173 us under a window of 250 and 481 under one of
+// everything, 0.44 and 0.53 of the fp32 matrix rate; 16 of 700, 8 heads of 64, window 250, 97, 0.39.
 template <int DIM>
 struct WindowF32Tile : MfmaF32Tile<DIM> {
     typedef MfmaF32Tile<DIM> Base;
