@@ -38,7 +38,7 @@
  *     lamps_validate_args checks all of this on request (it synchronises).
  *   - A context is not thread-safe; calls on it must be serialised -- with one
  *     exception: the compute-stream calls (lamps_decode_attn, lamps_kv_append,
- *     lamps_kv_append_tokens, lamps_prefill_attn, lamps_decode_attn_window,
+ *     lamps_kv_append_tokens, lamps_kv_read_tokens, lamps_prefill_attn, lamps_decode_attn_window,
  *     lamps_prefill_attn_window, lamps_rope_append, lamps_rope_append_tokens,
  *     lamps_batch_tables) read nothing of the context that ever changes, so ONE thread may make them while ONE other thread makes
  *     all the block-management and swap calls (alloc, free, swap, ticket, wait
@@ -79,6 +79,32 @@
  *     (16-byte runs that a wavefront loads coalesced and feeds to the matrix
  *     cores unchanged: 8 dims of one key; 4 consecutive slots of two dims of a
  *     value).  lamps_kv_layout() tells which one a configuration uses.
+ *
+ * A cache of 8 bits (LAMPS_E4M3)
+ *   Queries, outputs and the vectors that calls are given are bf16; the pools hold
+ *   e4m3 numbers (3 bits of fraction, exponents from -6, the largest 448; 127 and 255
+ *   are NaN), the codes, with one scale s for the keys and one for the values of each
+ *   (block, layer, kv head).  A code c stands for c * s, which is a bf16 number.
+ *       pool[num_blocks][num_layers][slice],  slice = num_kv_heads tiles of
+ *       block_size * head_dim bytes, then 8 * num_kv_heads bytes rounded up to 128
+ *   In the KEY pool these last hold float[num_kv_heads][2], the scales of keys and of
+ *   values of the block; in the value pool they are not used.  In a tile
+ *   (LAMPS_LAYOUT_CODES), with u, t as above and sub-tile base u * 16 * head_dim,
+ *         keys:    base + ((d / 16) * 16 + t) * 16 + d % 16
+ *         values:  base + (((d / 64) * 4 + t / 4) * 16 + d % 16) * 16 + ((d % 64) / 16) * 4 + t % 4
+ *   What an append makes of a block's new tokens, for keys and values apart:
+ *       n = 2^e, e the smallest whole number with |x| <= 448 * 2^e for all finite x of
+ *           them, held within [-110, 119]
+ *       s = n if the first of them is at slot 0, else the larger of n and the s that is
+ *           there; if that is n, codes at slots before them are rounded to it (to nearest
+ *           even, as everything here), c -> c * s_old / s
+ *       their codes are x / s, rounded; 448 where that is larger, NaN for what is no
+ *           finite number
+ *   So a block's scale grows with its tokens and begins anew with slot 0; a change of
+ *   scale is exact but for codes of the smallest sizes (below 2^-6 of the new scale).
+ *   A block's image in host memory has its scales with it.  part_tokens must be 0, and
+ *   lamps_rope_append and lamps_rope_append_tokens refuse such a cache; all other calls
+ *   take it.
  */
 #ifndef LAMPS_H
 #define LAMPS_H
@@ -92,8 +118,8 @@ extern "C" {
 
 typedef struct lamps_ctx lamps_ctx; /* opaque, library-owned */
 
-typedef enum { LAMPS_F32 = 0, LAMPS_BF16 = 1 } lamps_dtype;
-typedef enum { LAMPS_LAYOUT_PLAIN = 0, LAMPS_LAYOUT_TILED = 1 } lamps_layout;
+typedef enum { LAMPS_F32 = 0, LAMPS_BF16 = 1, LAMPS_E4M3 = 2 } lamps_dtype;
+typedef enum { LAMPS_LAYOUT_PLAIN = 0, LAMPS_LAYOUT_TILED = 1, LAMPS_LAYOUT_CODES = 2 } lamps_layout;
 
 typedef enum {
     LAMPS_OK = 0,
@@ -110,12 +136,13 @@ typedef struct {
     int32_t num_layers;         /* L >= 1                                            */
     int32_t num_q_heads;        /* H, a multiple of num_kv_heads                     */
     int32_t num_kv_heads;       /* H_kv; query head h reads kv head h / (H / H_kv)   */
-    int32_t head_dim;           /* d_h: bf16 {64,128,256}, f32 {32,64,128}           */
+    int32_t head_dim;           /* d_h: bf16 and e4m3 {64,128,256}, f32 {32,64,128}  */
     int32_t block_size;         /* tokens per block, a power of two >= 16            */
     int32_t num_blocks;         /* physical blocks in each pool                      */
     int32_t max_blocks_per_req; /* row length of the block table                     */
     int32_t max_batch;          /* largest `batch` passed to lamps_decode_attn       */
-    int32_t dtype;              /* lamps_dtype of q, the pools and out               */
+    int32_t dtype;              /* lamps_dtype of q, the pools and out (LAMPS_E4M3:
+                                   of the pools; q and out are bf16)                 */
     float softmax_scale;        /* 0 => 1/sqrt(head_dim), the Section 2.2 equation   */
     int32_t part_tokens;        /* 0 => by the sizes of each call (default: all cached
                                    tokens are dealt out evenly); > 0 => fixed
@@ -154,7 +181,8 @@ typedef struct {
 /* ---- sizes (pure functions of the config; return 0 on an invalid config) ---- */
 
 /* M of equations (1)-(3): bytes of KV cache per token over all layers,
- * 2 * L * H_kv * d_h * sizeof(dtype) (Section 2.2.1). */
+ * 2 * L * H_kv * d_h * sizeof(dtype) (Section 2.2.1); LAMPS_E4M3: a block's bytes by
+ * its tokens, rounded up (1.008 times 2 * L * H_kv * d_h at 8 heads of 128, blocks of 16). */
 size_t lamps_kv_bytes_per_token(const lamps_config *cfg);
 /* lamps_layout of the tiles of both pools for this configuration (see the
  * layout section above), or LAMPS_ERR_INVALID. */
@@ -309,6 +337,17 @@ int lamps_kv_append(lamps_ctx *ctx, int32_t layer, int32_t batch, const void *k_
 int lamps_kv_append_tokens(lamps_ctx *ctx, int32_t layer, int32_t n_req, int32_t total_tokens,
                            const void *k_new, const void *v_new, const int32_t *q_start,
                            const int32_t *block_table, const int32_t *ctx_lens);
+/* The reverse: the keys and values of those positions out of the cache, as rows.
+ * Positions and rows are as above (the LAST q_start[r+1] - q_start[r] positions of each
+ * request), and so is what is ignored; rows of what is not read, and rows past
+ * q_start[n_req], are left as they were.  LAMPS_E4M3: what the codes stand for, exactly;
+ * other types: what was appended, bit for bit.
+ *   k_out, v_out  device, [total_tokens][H_kv][d_h] dtype (LAMPS_E4M3: bf16), 16-byte
+ *                 aligned, not overlapping
+ * Errors: INVALID (null, alignment, overlap), RANGE (layer, n_req > max_batch, negative sizes). */
+int lamps_kv_read_tokens(lamps_ctx *ctx, int32_t layer, int32_t n_req, int32_t total_tokens,
+                         const int32_t *q_start, const int32_t *block_table,
+                         const int32_t *ctx_lens, void *k_out, void *v_out);
 /* Attention of every new token over the cached positions up to and including
  * its own (the Section 2.2 equation per token; the new tokens' keys and values
  * must already be in the cache):

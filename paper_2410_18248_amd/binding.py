@@ -7,8 +7,8 @@ library's kernels, and there is no fallback if the library is missing.
 import ctypes
 import os
 
-LAMPS_F32, LAMPS_BF16 = 0, 1
-LAMPS_LAYOUT_PLAIN, LAMPS_LAYOUT_TILED = 0, 1
+LAMPS_F32, LAMPS_BF16, LAMPS_E4M3 = 0, 1, 2
+LAMPS_LAYOUT_PLAIN, LAMPS_LAYOUT_TILED, LAMPS_LAYOUT_CODES = 0, 1, 2
 LAMPS_ROPE_HALVES, LAMPS_ROPE_NEIGHBOURS = 0, 1
 LAMPS_ROPE_UNSCALED, LAMPS_ROPE_LINEAR, LAMPS_ROPE_BASE, LAMPS_ROPE_BY_PARTS = range(4)
 
@@ -117,6 +117,7 @@ def load_library():
         "lamps_validate_args": [vp, i32, vp, vp, vp, vp],
         "lamps_kv_append": [vp, i32, i32, vp, vp, vp, vp, vp, i32],
         "lamps_kv_append_tokens": [vp, i32, i32, i32, vp, vp, vp, vp, vp],
+        "lamps_kv_read_tokens": [vp, i32, i32, i32, vp, vp, vp, vp, vp],
         "lamps_prefill_attn": [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp],
         "lamps_decode_attn_window": [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp],
         "lamps_prefill_attn_window": [vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp],
@@ -406,6 +407,10 @@ class Lamps:
         self._check(self.lib.lamps_kv_append_tokens(self.h, layer, n_req, total_tokens, _ptr(k_new),
                                                     _ptr(v_new), _ptr(q_start), _ptr(block_table),
                                                     _ptr(ctx_lens)))
+
+    def kv_read_tokens(self, layer, n_req, total_tokens, q_start, block_table, ctx_lens, k_out, v_out):
+        self._check(self.lib.lamps_kv_read_tokens(self.h, layer, n_req, total_tokens, _ptr(q_start), _ptr(block_table),
+                                                  _ptr(ctx_lens), _ptr(k_out), _ptr(v_out)))
 
     def prefill_attn(self, layer, n_req, total_tokens, q, q_start, block_table, ctx_lens, out,
                      max_new_tokens=0):

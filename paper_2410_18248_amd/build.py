@@ -26,7 +26,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblamps.so")
 SOURCES = ["decode_attn.hip", "block_copy.hip", "kv_append.hip", "prefill_attn.hip", "window_attn.hip", "rope_append.hip",
-           "batch_tables.hip", "validate.hip", "lamps.cpp", "sched.cpp"]
+           "batch_tables.hip", "kv8_append.hip", "kv8_decode.hip", "kv8_prefill.hip", "validate.hip", "lamps.cpp", "sched.cpp"]
 # the scheduler's times are compared bit for bit with a plain evaluation of the same formulas:
 # no fused multiply-adds in its host code
 PER_SOURCE = {"sched.cpp": ["-ffp-contract=off"],
@@ -36,7 +36,9 @@ PER_SOURCE = {"sched.cpp": ["-ffp-contract=off"],
               # every 30-47 (measured)
               "decode_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
               "prefill_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-              "window_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+              "window_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+              "kv8_decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+              "kv8_prefill.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",

@@ -1381,6 +1381,13 @@ extern "C" int lamps_decode_attn_static(const lamps_config *cfg, void *compute_s
     a.partials = reinterpret_cast<float *>(base);
     a.partial_capacity = lamps::kStaticPartialBytes;
     a.share_info = reinterpret_cast<int4 *>(base + lamps::kStaticPartialBytes);
+    if (cfg->dtype == LAMPS_E4M3) {
+        lamps::WindowArgs w{};
+        w.d = a;
+        w.window = lamps::kEverything;
+        e = lamps::launch_kv8_decode(w, static_cast<hipStream_t>(compute_stream));
+        return e == hipSuccess ? (int)LAMPS_OK : static_fail(LAMPS_ERR_HIP, hipGetErrorString(e));
+    }
     size_t demand = 0;
     if ((e = lamps::dispatch(a, nullptr, &demand)) != hipSuccess)
         return static_fail(LAMPS_ERR_HIP, hipGetErrorString(e));

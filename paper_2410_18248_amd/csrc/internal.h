@@ -79,6 +79,15 @@ hipError_t launch_kv_append(AppendArgs a, int tiled, hipStream_t stream);
 // of request r's context.
 hipError_t launch_kv_append_tokens(const AppendArgs &a, int total_tokens, int tiled, hipStream_t stream);
 
+// The same two for a cache of 8 bits (k_new, v_new are bf16), and its reverse: the last q_start[r + 1] - q_start[r] positions of each request as rows of
+// the calls' own type; form: lamps_layout of the pools.
+struct CodesArgs : AppendArgs {
+    int32_t total_tokens;
+};
+hipError_t launch_kv8_append(const AppendArgs &a, hipStream_t stream);
+hipError_t launch_kv8_append_tokens(const CodesArgs &a, hipStream_t stream);
+hipError_t launch_kv_read_tokens(const CodesArgs &a, int form, void *k_out, void *v_out, hipStream_t stream);
+
 struct PrefillArgs {
     DecodeArgs d;                // q and out are [total_tokens][H][D]; batch = number of requests
     const int32_t *q_start;      // [batch + 1]
@@ -106,6 +115,11 @@ struct WindowArgs {
 };
 hipError_t launch_decode_window(const WindowArgs &a, hipStream_t stream);
 hipError_t launch_prefill_window(const WindowArgs &a, hipStream_t stream);
+
+// The same for a cache of 8 bits.  Without a window, it is kEverything.
+constexpr int32_t kEverything = 1 << 30;     // (no row has more positions)
+hipError_t launch_kv8_decode(const WindowArgs &a, hipStream_t stream);
+hipError_t launch_kv8_prefill(const WindowArgs &a, hipStream_t stream);
 
 struct RopeArgs {
     const void *q, *k_new, *v_new;   // rows of [H or H_kv][D], the strides apart

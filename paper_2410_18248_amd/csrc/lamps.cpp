@@ -47,12 +47,12 @@ struct Derived {
 const char *derive(const lamps_config *c, Derived *d)
 {
     if (!c) return "config is null";
-    if (c->dtype != LAMPS_F32 && c->dtype != LAMPS_BF16) return "dtype must be LAMPS_F32 or LAMPS_BF16";
+    if (c->dtype != LAMPS_F32 && c->dtype != LAMPS_BF16 && c->dtype != LAMPS_E4M3) return "dtype must be LAMPS_F32, LAMPS_BF16 or LAMPS_E4M3";
     if (c->num_layers < 1 || c->num_q_heads < 1 || c->num_kv_heads < 1 || c->head_dim < 1 ||
         c->num_blocks < 1 || c->max_blocks_per_req < 1 || c->max_batch < 1)
         return "sizes must be positive";
     if (c->num_q_heads % c->num_kv_heads != 0) return "num_q_heads must be a multiple of num_kv_heads";
-    const int bf16 = c->dtype == LAMPS_BF16;
+    const int bf16 = c->dtype != LAMPS_F32;     // (of queries and outputs)
     if (lamps::decode_heads_per_pass(bf16, c->head_dim, c->num_q_heads / c->num_kv_heads) == 0)
         return "unsupported head_dim for this dtype (bf16: 64/128/256, f32: 32/64/128)";
     if (c->block_size < 16 || (c->block_size & (c->block_size - 1)) != 0)
@@ -61,12 +61,17 @@ const char *derive(const lamps_config *c, Derived *d)
     d->elem = bf16 ? 2 : 4;
     d->log2_bs = 0;
     while ((1 << d->log2_bs) < c->block_size) ++d->log2_bs;
-    d->half_bytes = (size_t)c->num_layers * c->num_kv_heads * c->block_size * c->head_dim * d->elem;
+    // of one block, one layer and pool: the heads' tiles, and of a cache of 8 bits room for their scales behind them
+    const size_t layer_bytes = c->dtype == LAMPS_E4M3
+                                   ? (size_t)c->num_kv_heads * c->block_size * c->head_dim + (((size_t)c->num_kv_heads * 8 + 127) & ~(size_t)127)
+                                   : (size_t)c->num_kv_heads * c->block_size * c->head_dim * d->elem;
+    d->half_bytes = c->num_layers * layer_bytes;
     d->block_bytes = 2 * d->half_bytes;
     d->pool_bytes = d->half_bytes * (size_t)c->num_blocks;
     d->part_tokens = c->part_tokens;
     if (d->part_tokens < 0 || d->part_tokens % c->block_size != 0)
         return "part_tokens must be 0 or a positive multiple of block_size";
+    if (d->part_tokens > 0 && c->dtype == LAMPS_E4M3) return "part_tokens must be 0 with LAMPS_E4M3";
     if (c->max_batch > 8192) return "max_batch is limited to 8192";
     const int group = c->num_q_heads / c->num_kv_heads;
     const int gh = lamps::decode_heads_per_pass(bf16, c->head_dim, group);
@@ -169,7 +174,7 @@ void fill_geometry(const lamps_config &cfg, const Derived &d, lamps::DecodeArgs 
     a.num_blocks = cfg.num_blocks;
     a.part_tokens = d.part_tokens;
     a.max_parts = d.max_parts;
-    a.bf16 = cfg.dtype == LAMPS_BF16;
+    a.bf16 = cfg.dtype != LAMPS_F32;
     a.heads_per_pass = lamps::decode_heads_per_pass(a.bf16, a.head_dim, a.num_q_heads / a.num_kv_heads);
     a.passes = a.num_q_heads / a.num_kv_heads / a.heads_per_pass;
     a.scale_log2e = d.scale_log2e;
@@ -258,7 +263,7 @@ const char *fill_rope_args(lamps_ctx *c, lamps::RopeArgs *pa, int32_t layer, int
     a.advance = 0;
     a.total_tokens = rows;
     a.batch = batch;
-    a.bf16 = g.dtype == LAMPS_BF16;
+    a.bf16 = g.dtype != LAMPS_F32;
     a.layer = layer;
     a.num_layers = g.num_layers;
     a.num_q_heads = g.num_q_heads;
@@ -617,6 +622,7 @@ size_t lamps_kv_bytes_per_token(const lamps_config *cfg)
 {
     Derived d;
     if (derive(cfg, &d)) return 0;
+    if (cfg->dtype == LAMPS_E4M3) return (d.block_bytes + cfg->block_size - 1) / cfg->block_size;
     return 2 * (size_t)cfg->num_layers * cfg->num_kv_heads * cfg->head_dim * d.elem;
 }
 
@@ -625,6 +631,7 @@ int lamps_kv_layout(const lamps_config *cfg)
     try {
         Derived d;
         if (derive(cfg, &d)) return LAMPS_ERR_INVALID;
+        if (cfg->dtype == LAMPS_E4M3) return LAMPS_LAYOUT_CODES;
         return lamps::decode_uses_tiled_layout(cfg->dtype == LAMPS_BF16, cfg->num_q_heads / cfg->num_kv_heads)
                    ? LAMPS_LAYOUT_TILED
                    : LAMPS_LAYOUT_PLAIN;
@@ -739,6 +746,13 @@ int lamps_decode_attn(lamps_ctx *c, int32_t layer, int32_t batch, const void *q,
         if (batch == 0) return LAMPS_OK;
         lamps::DecodeArgs a;
         fill_decode_args(c, &a, layer, batch, q, block_table, ctx_lens, running_mask, out);
+        if (c->cfg.dtype == LAMPS_E4M3) {
+            lamps::WindowArgs w{};
+            w.d = a;
+            w.window = lamps::kEverything;
+            LAMPS_HIP(lamps::launch_kv8_decode(w, c->cs));
+            return LAMPS_OK;
+        }
         LAMPS_HIP(lamps::launch_decode(a, c->cs));
         return LAMPS_OK;
     }
@@ -806,8 +820,12 @@ int lamps_kv_append(lamps_ctx *c, int32_t layer, int32_t batch, const void *k_ne
         a.log2_block_size = c->d.log2_bs;
         a.max_blocks = c->cfg.max_blocks_per_req;
         a.num_blocks = c->cfg.num_blocks;
-        a.bf16 = c->cfg.dtype == LAMPS_BF16;
+        a.bf16 = c->cfg.dtype != LAMPS_F32;
         a.advance = advance != 0;
+        if (c->cfg.dtype == LAMPS_E4M3) {
+            LAMPS_HIP(lamps::launch_kv8_append(a, c->cs));
+            return LAMPS_OK;
+        }
         const int tiled = lamps::decode_uses_tiled_layout(a.bf16, c->cfg.num_q_heads / c->cfg.num_kv_heads);
         LAMPS_HIP(lamps::launch_kv_append(a, tiled, c->cs));
         return LAMPS_OK;
@@ -830,7 +848,7 @@ int lamps_kv_append_tokens(lamps_ctx *c, int32_t layer, int32_t n_req, int32_t t
         if (n_req < 0 || n_req > c->cfg.max_batch || total_tokens < 0)
             return fail(c, LAMPS_ERR_RANGE, "lamps_kv_append_tokens: n_req / total_tokens out of range");
         if (n_req == 0 || total_tokens == 0) return LAMPS_OK;
-        lamps::AppendArgs a;
+        lamps::CodesArgs a;
         a.k_new = k_new;
         a.v_new = v_new;
         a.k_pool = c->k_pool;
@@ -848,10 +866,58 @@ int lamps_kv_append_tokens(lamps_ctx *c, int32_t layer, int32_t n_req, int32_t t
         a.log2_block_size = c->d.log2_bs;
         a.max_blocks = c->cfg.max_blocks_per_req;
         a.num_blocks = c->cfg.num_blocks;
-        a.bf16 = c->cfg.dtype == LAMPS_BF16;
+        a.bf16 = c->cfg.dtype != LAMPS_F32;
         a.advance = 0;
+        a.total_tokens = total_tokens;
+        if (c->cfg.dtype == LAMPS_E4M3) {
+            LAMPS_HIP(lamps::launch_kv8_append_tokens(a, c->cs));
+            return LAMPS_OK;
+        }
         const int tiled = lamps::decode_uses_tiled_layout(a.bf16, c->cfg.num_q_heads / c->cfg.num_kv_heads);
         LAMPS_HIP(lamps::launch_kv_append_tokens(a, total_tokens, tiled, c->cs));
+        return LAMPS_OK;
+    }
+    LAMPS_CATCH(c)
+}
+
+int lamps_kv_read_tokens(lamps_ctx *c, int32_t layer, int32_t n_req, int32_t total_tokens, const int32_t *q_start,
+                         const int32_t *block_table, const int32_t *ctx_lens, void *k_out, void *v_out)
+{
+    try {
+        if (!c) return LAMPS_ERR_INVALID;
+        if (!q_start || !block_table || !ctx_lens || !k_out || !v_out)
+            return fail(c, LAMPS_ERR_INVALID, "lamps_kv_read_tokens: null argument");
+        if (((uintptr_t)k_out | (uintptr_t)v_out) & 15)
+            return fail(c, LAMPS_ERR_INVALID, "lamps_kv_read_tokens: k_out and v_out must be 16-byte aligned");
+        const size_t rows = total_tokens > 0 ? (size_t)total_tokens * c->cfg.num_kv_heads * c->cfg.head_dim * c->d.elem : 0;
+        if (overlap(k_out, rows, v_out, rows)) return fail(c, LAMPS_ERR_INVALID, "lamps_kv_read_tokens: k_out and v_out overlap");
+        if (layer < 0 || layer >= c->cfg.num_layers)
+            return fail(c, LAMPS_ERR_RANGE, "lamps_kv_read_tokens: layer out of range");
+        if (n_req < 0 || n_req > c->cfg.max_batch || total_tokens < 0)
+            return fail(c, LAMPS_ERR_RANGE, "lamps_kv_read_tokens: n_req / total_tokens out of range");
+        if (n_req == 0 || total_tokens == 0) return LAMPS_OK;
+        lamps::CodesArgs a;
+        a.k_new = a.v_new = nullptr;
+        a.k_pool = c->k_pool;
+        a.v_pool = c->v_pool;
+        a.block_table = block_table;
+        a.ctx_lens = const_cast<int32_t *>(ctx_lens);     // (only read)
+        a.running = nullptr;
+        a.q_start = q_start;
+        a.batch = n_req;
+        a.layer = layer;
+        a.num_layers = c->cfg.num_layers;
+        a.num_kv_heads = c->cfg.num_kv_heads;
+        a.head_dim = c->cfg.head_dim;
+        a.block_size = c->cfg.block_size;
+        a.log2_block_size = c->d.log2_bs;
+        a.max_blocks = c->cfg.max_blocks_per_req;
+        a.num_blocks = c->cfg.num_blocks;
+        a.bf16 = c->cfg.dtype != LAMPS_F32;
+        a.advance = 0;
+        a.slices = 1;
+        a.total_tokens = total_tokens;
+        LAMPS_HIP(lamps::launch_kv_read_tokens(a, lamps_kv_layout(&c->cfg), k_out, v_out, c->cs));
         return LAMPS_OK;
     }
     LAMPS_CATCH(c)
@@ -879,6 +945,18 @@ int lamps_prefill_attn(lamps_ctx *c, int32_t layer, int32_t n_req, int32_t total
         p.max_new_tokens = max_new_tokens > 0 && max_new_tokens < total_tokens ? max_new_tokens : total_tokens;
         p.force_rows = max_new_tokens < 0;
         p.tag = lamps::next_launch_tag();
+        if (c->cfg.dtype == LAMPS_E4M3) {
+            lamps::WindowArgs w{};
+            w.d = p.d;
+            w.q_start = q_start;
+            w.window = lamps::kEverything;
+            w.total_tokens = p.total_tokens;
+            w.max_new_tokens = p.max_new_tokens;
+            w.force_rows = p.force_rows;
+            w.tag = p.tag;
+            LAMPS_HIP(lamps::launch_kv8_prefill(w, c->cs));
+            return LAMPS_OK;
+        }
         LAMPS_HIP(lamps::launch_prefill(p, c->cs));
         return LAMPS_OK;
     }
@@ -903,9 +981,9 @@ int lamps_decode_attn_window(lamps_ctx *c, int32_t layer, int32_t batch, int32_t
         if (batch == 0) return LAMPS_OK;
         lamps::WindowArgs w = {};
         fill_decode_args(c, &w.d, layer, batch, q, block_table, ctx_lens, running_mask, out);
-        w.window = std::min(window, 1 << 30);             // (no row has more positions)
-        w.sinks = std::min(sinks, 1 << 30);
-        LAMPS_HIP(lamps::launch_decode_window(w, c->cs));
+        w.window = std::min(window, lamps::kEverything);
+        w.sinks = std::min(sinks, lamps::kEverything);
+        LAMPS_HIP(c->cfg.dtype == LAMPS_E4M3 ? lamps::launch_kv8_decode(w, c->cs) : lamps::launch_decode_window(w, c->cs));
         return LAMPS_OK;
     }
     LAMPS_CATCH(c)
@@ -931,13 +1009,13 @@ int lamps_prefill_attn_window(lamps_ctx *c, int32_t layer, int32_t n_req, int32_
         lamps::WindowArgs w = {};
         fill_decode_args(c, &w.d, layer, n_req, q, block_table, ctx_lens, nullptr, out);
         w.q_start = q_start;
-        w.window = std::min(window, 1 << 30);             // (no row has more positions)
-        w.sinks = std::min(sinks, 1 << 30);
+        w.window = std::min(window, lamps::kEverything);
+        w.sinks = std::min(sinks, lamps::kEverything);
         w.total_tokens = total_tokens;
         w.max_new_tokens = max_new_tokens > 0 && max_new_tokens < total_tokens ? max_new_tokens : total_tokens;
         w.force_rows = max_new_tokens < 0;
         w.tag = lamps::next_launch_tag();
-        LAMPS_HIP(lamps::launch_prefill_window(w, c->cs));
+        LAMPS_HIP(c->cfg.dtype == LAMPS_E4M3 ? lamps::launch_kv8_prefill(w, c->cs) : lamps::launch_prefill_window(w, c->cs));
         return LAMPS_OK;
     }
     LAMPS_CATCH(c)
@@ -978,6 +1056,7 @@ int lamps_rope_append(lamps_ctx *c, int32_t layer, int32_t batch, const lamps_ro
         lamps::RopeArgs a = {};
         const char *text = fill_rope_args(c, &a, layer, batch, batch, rope, q, q_stride, k_new, k_stride, v_new, v_stride, block_table, ctx_lens, q_out);
         if (!text && !running_mask) text = "null argument";
+        if (!text && c->cfg.dtype == LAMPS_E4M3) text = "not into a cache of 8 bits";
         if (text) return fail(c, LAMPS_ERR_INVALID, std::string("lamps_rope_append: ") + text);
         if (layer < 0 || layer >= c->cfg.num_layers)
             return fail(c, LAMPS_ERR_RANGE, "lamps_rope_append: layer out of range");
@@ -1002,6 +1081,7 @@ int lamps_rope_append_tokens(lamps_ctx *c, int32_t layer, int32_t n_req, int32_t
         lamps::RopeArgs a = {};
         const char *text = fill_rope_args(c, &a, layer, n_req, total_tokens, rope, q, q_stride, k_new, k_stride, v_new, v_stride, block_table, ctx_lens, q_out);
         if (!text && !q_start) text = "null argument";
+        if (!text && c->cfg.dtype == LAMPS_E4M3) text = "not into a cache of 8 bits";
         if (text) return fail(c, LAMPS_ERR_INVALID, std::string("lamps_rope_append_tokens: ") + text);
         if (layer < 0 || layer >= c->cfg.num_layers)
             return fail(c, LAMPS_ERR_RANGE, "lamps_rope_append_tokens: layer out of range");
