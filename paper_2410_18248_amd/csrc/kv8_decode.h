@@ -9,6 +9,13 @@ typedef __attribute__((address_space(4))) const uint64_t *scales_ptr;   // read-
 
 __device__ __forceinline__ bf16x8 operand(uint32_t x, uint32_t y, uint32_t z, uint32_t w) { return __builtin_bit_cast(bf16x8, make_uint4(x, y, z, w)); }
 
+// Where the two sub-tiles of the unit at t are read: one that nothing is seen of, whose block may be anyone's, in the other one's place.
+__device__ __forceinline__ int2 sub_tiles(const Sight<32> &see, int t)
+{
+    const bool first = (t + 15 >= see.lo) | (t < see.sinks), second = (t + 16 < see.end) & ((t + 31 >= see.lo) | (t + 16 < see.sinks));
+    return make_int2(first ? t : t + 16, second ? t + 16 : t);
+}
+
 // As MfmaReducer, with codes for operands: a lane's 16 bytes are 16 dims of a key, two operands of 16x16x32 products (the contraction
 // index is permuted, and the queries with it), or four positions of four values' dims, which with the four of the unit's other sub-tile are the
 // operands of four products over 32 positions.  A unit of 32 positions is two sub-tiles of 16, in one block or two, each with its block's scales, which
@@ -47,19 +54,18 @@ struct CodesReducer {
         const char *k0 = static_cast<const char *>(a.k_pool) + a.layer * slice;
         const char *kp = k0 + g * tile + lane * 16, *vp = static_cast<const char *>(a.v_pool) + a.layer * slice + g * tile + lane * 16;
         const char *sp = k0 + a.num_kv_heads * tile + g * 8;
-        const int last = a.max_blocks * a.block_size - 1;
         const auto place = [&](int c) { return see.at(u0 + min(c, n - 1)); };
         const auto entry = [&](int c) {
-            const int t = place(c);
-            return make_int2(table[t >> a.log2_block_size], table[min(t + 16, last) >> a.log2_block_size]);
+            const int2 t = sub_tiles(see, place(c));
+            return make_int2(table[t.x >> a.log2_block_size], table[t.y >> a.log2_block_size]);
         };
         const auto issue = [&](int c, int2 blocks, Unit &x) {
-            const int t = place(c);
+            const int2 t = sub_tiles(see, place(c));
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 // (an entry that names no block of the pool reads the last one; the row is meaningless)
                 const size_t block = (size_t)min((unsigned)(h ? blocks.y : blocks.x), (unsigned)a.num_blocks - 1) * stride;
-                const size_t off = block + (size_t)(((t + 16 * h) & (a.block_size - 1)) >> 4) * (16 * D);
+                const size_t off = block + (size_t)(((h ? t.y : t.x) & (a.block_size - 1)) >> 4) * (16 * D);
                 x.scale[h] = __builtin_bit_cast(float2, *(scales_ptr)(uintptr_t)(sp + block));
 #pragma unroll
                 for (int i = 0; i < NL; ++i) x.k[h][i] = load_stream16(kp + off + i * 1024);

@@ -1,4 +1,529 @@
+// Attention of many new tokens per request over a cache of 8 bits, everything up to each one's own position or a window of it and its first positions.
+//
+//   out[n] = softmax(q[n] K^T * scale) V  over the positions t <= p with t > p - window or t < sinks, K and V the numbers that the codes stand for
+//
+// One workgroup = one (request, kv head, tile of new tokens), or one of the parts of its walk: four waves of kCB blocks of 16 columns, (new token, head-of-group)
+// pairs.  A stage is 32 cached positions: their codes are converted once, on the way into LDS, by all four waves, to the operands of the
+// products that every wave reads (by each wave for itself it would be 64 conversions a stage and wave at head size 128, half as much again as the softmax takes of the
+// vector ALUs).  Codes of the next stage but one are in registers meanwhile.  The softmax keeps a running maximum that moves only
+// where a weight would pass 2^8; weights are rounded to bf16 for the second product and summed as rounded.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "attn_reducers.h"
+#include "handover.h"
 #include "internal.h"
+#include "kv8.h"
+#include "requests.h"
+#include "tile_parts.h"
+#include "kv8_decode.h"
+
 namespace lamps {
-hipError_t launch_kv8_prefill(const WindowArgs &, hipStream_t) { return hipErrorInvalidValue; }
+namespace {
+
+struct Tiling {
+    int items;                                           // workgroups of a head
+    int places;                                          // workgroups that all work is dealt to evenly where requests are cut; 0: none is
+};
+constexpr int kMostRequests = 256;                       // of a launch that cuts
+constexpr int kLeastStages = 8;                          // of a part
+
+// What a workgroup takes.
+struct TilePiece {
+    int r, g, tile, first, n_new, ctx;                   // the tile's tokens: rows first + tile * WT and up of n_new
+    int runs, at, item;                                  // part `at` of up to `runs`; the item of the first
+};
+
+// With a place for every part: each wave holds all requests, K to a lane.  What is cut comes first.
+template <int K>
+__device__ __forceinline__ bool find_tile(const WindowArgs &w, const Tiling &c, int WT, int piece, TilePiece &x)
+{
+    const DecodeArgs &a = w.d;
+    const int lane = threadIdx.x & 63;
+    int first[K], count[K], ctx[K], tiles[K], stages[K], own[K], mine[2] = {0, 0};
+    float work = 0.0f;
+    int longest = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int i = min(K * lane + k, a.batch - 1);
+        first[k] = w.q_start[i];
+        count[k] = w.q_start[i + 1];
+        ctx[k] = a.ctx_lens[i];
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        count[k] -= first[k];
+        // (a context shorter than its new tokens, or longer than the table row: nothing is read or written for it; rows past the last: none)
+        const bool on = K * lane + k < a.batch && first[k] >= 0 && count[k] > 0 && ctx[k] >= count[k] && ctx[k] <= a.max_blocks * a.block_size;
+        const int rows = on ? min(count[k], w.total_tokens - first[k]) : 0;
+        tiles[k] = max(0, (rows + WT - 1) / WT);
+        const int p = ctx[k] - count[k] + rows;          // (the last tile's end, and what its first token sees)
+        stages[k] = tiles[k] > 0 ? Sight<32>(p, max(0, p - min(rows, WT) - w.window + 1), w.sinks, std::true_type{}).units : 0;
+        work += (float)stages[k] * (float)tiles[k];
+        longest = max(longest, stages[k]);
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) work += __shfl_xor(work, s);
+    longest = __builtin_amdgcn_readlane(wave_max_to(longest), 63);
+    // an even share (the sum is off by a few times 2^-24)
+    const float even = work * (float)a.num_kv_heads / (float)c.places * 1.00001f + 1.0f;
+    const int size = max(kLeastStages, even < (float)(1 << 26) ? (int)even : 1 << 26), worth = size + size / 2;
+    // the cut requests' pieces, then the others'
+    bool cut[K];
+    int runs[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        cut[k] = stages[k] > worth;
+        runs[k] = cut[k] ? (int)((unsigned)(stages[k] + size - 1) / (unsigned)size) : 1;
+        own[k] = tiles[k] * runs[k];
+        mine[cut[k] ? 0 : 1] += own[k];
+    }
+    const int upto_cut = wave_scan(mine[0]), cuts = __builtin_amdgcn_readlane(upto_cut, 63);
+    const bool in_cuts = piece < cuts;
+    const int upto = in_cuts ? upto_cut : wave_scan(mine[1]) + cuts;
+    if (piece >= __builtin_amdgcn_readlane(upto, 63)) return false;
+    const int l = __popcll(__ballot(upto <= piece));
+    int at = piece - __builtin_amdgcn_readlane(upto - (in_cuts ? mine[0] : mine[1]), l);
+    bool found = false;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int n = __builtin_amdgcn_readlane(cut[k] == in_cuts ? own[k] : 0, l);
+        if (!found && at < n) {
+            found = true;
+            x.r = K * l + k;
+            x.first = __builtin_amdgcn_readlane(first[k], l);
+            x.n_new = __builtin_amdgcn_readlane(count[k], l);
+            x.ctx = __builtin_amdgcn_readlane(ctx[k], l);
+            x.runs = __builtin_amdgcn_readlane(runs[k], l);
+            const int t = (int)((unsigned)at / (unsigned)x.runs), all = __builtin_amdgcn_readlane(tiles[k], l);
+            x.at = at - t * x.runs;
+            x.item = piece - x.at;
+            x.tile = all - 1 - t;                        // (the longest first)
+        } else if (!found) {
+            at -= n;
+        }
+    }
+    return found;
 }
+
+// Without: any number of requests, none cut.
+__device__ __forceinline__ bool find_whole_tile(const WindowArgs &w, int WT, int piece, TilePiece &x)
+{
+    const DecodeArgs &a = w.d;
+    const NewTokens n = new_tokens_at(w.q_start, a.ctx_lens, a.batch, piece, [WT](int q, int r) { return q / WT + r; });
+    x.r = __builtin_amdgcn_readfirstlane(n.r);
+    x.first = __builtin_amdgcn_readfirstlane(n.first);
+    x.n_new = __builtin_amdgcn_readfirstlane(n.count);
+    x.ctx = __builtin_amdgcn_readfirstlane(n.ctx);
+    x.tile = __builtin_amdgcn_readfirstlane(piece - (x.first / WT + x.r));
+    x.runs = 1;
+    x.at = 0;
+    x.item = piece;
+    if (x.first < 0 || x.tile < 0 || x.ctx < x.n_new || x.ctx > a.max_blocks * a.block_size) return false;
+    return (long long)x.tile * WT < min(x.n_new, w.total_tokens - x.first);
+}
+
+constexpr size_t tile_state(int D, int columns) { return (size_t)columns * (D + 2); }   // floats
+
+template <int D, int kCB>
+__global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_tiles(const WindowArgs w, const Tiling c)
+{
+    constexpr int kCols = 16 * kCB, NK = D / 32, NS = D / 16, LPT = D / 64;
+    constexpr int SUBK = 16 * D * 2, VOFF = 2 * SUBK, STAGE = 4 * SUBK;   // bytes of a sub-tile of keys, where values begin, of a stage
+    constexpr bool kEarly = D <= 64 || (D == 128 && kCB == 1);   // values are asked for in front of the softmax: where registers hold them
+    __shared__ __align__(16) char lds[2 * STAGE];
+    __shared__ uint32_t wild_at[2][kWaves];
+
+    const DecodeArgs &a = w.d;
+    const int G = a.num_q_heads / a.num_kv_heads, TW = kCols / G, WT = kWaves * TW;
+    TilePiece at;
+    // (heads next to each other: with 8 of them and more all tiles of one go to one XCD, whose L2 has its keys and values)
+    const int piece = (int)((unsigned)blockIdx.x / (unsigned)a.num_kv_heads);
+    at.g = blockIdx.x - piece * a.num_kv_heads;
+    if (c.places == 0 ? !find_whole_tile(w, WT, piece, at) : a.batch <= 64 ? !find_tile<1>(w, c, WT, piece, at) : !find_tile<4>(w, c, WT, piece, at)) return;
+    const int g = at.g, first = at.first, base_pos = at.ctx - at.n_new, n_new = min(at.n_new, w.total_tokens - first);
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 15, qd = lane >> 4;
+
+    // what the tile walks over, and the part of it that is this workgroup's
+    const int p_first = base_pos + at.tile * WT, p_last = base_pos + min(n_new, (at.tile + 1) * WT) - 1;
+    const Sight<32> see(p_last + 1, max(0, p_first - w.window + 1), w.sinks, std::true_type{});
+    int st0 = 0, st1 = see.units, runs = 1;
+    if (at.runs > 1) {
+        // (a tile of earlier tokens may have less than the request's last one, by which the parts are counted)
+        const int want = max(1, min(at.runs, see.units / (kLeastStages / 2))), each = (see.units + want - 1) / want;
+        runs = (see.units + each - 1) / each;
+        if (at.at >= runs) return;
+        st0 = at.at * each;
+        st1 = min(see.units, st0 + each);
+    }
+    // the wave's own tokens; none: positions that see nothing
+    const int wave_tok = at.tile * WT + wv * TW;
+    const bool none = wave_tok >= n_new;
+    const int wave_min = __builtin_amdgcn_readfirstlane(none ? 0x3fffffff : base_pos + wave_tok);
+    const int wave_max = __builtin_amdgcn_readfirstlane(none ? -1 : base_pos + min(n_new, wave_tok + TW) - 1);
+    const int wave_hi = wave_max - w.window + 1, wave_lo = wave_min - w.window + 1;   // where the windows of the wave's last and first token begin
+
+    const table_ptr table = (table_ptr)(uintptr_t)(a.block_table + (size_t)at.r * a.max_blocks);
+    const size_t tile_bytes = (size_t)a.block_size * D, slice = codes_slice(a.num_kv_heads, a.block_size, D), stride = a.num_layers * slice;
+    const char *k0 = static_cast<const char *>(a.k_pool) + a.layer * slice;
+    const char *kp = k0 + g * tile_bytes, *vp = static_cast<const char *>(a.v_pool) + a.layer * slice + g * tile_bytes;
+    const char *sp = k0 + a.num_kv_heads * tile_bytes + g * 8;
+    const int last_pos = a.max_blocks * a.block_size - 1, last_stage = see.units - 1;
+    const auto lookup = [&](int st) {
+        const int2 t = sub_tiles(see, see.at(min(st, last_stage)));
+        return make_int2(table[t.x >> a.log2_block_size], table[t.y >> a.log2_block_size]);
+    };
+    // This thread's units of a stage, 16 bytes of codes: units of keys of both sub-tiles, then of values.  All of a wave's are of one kind and sub-tile.
+    uint4 raw[LPT];
+    float scale_of[LPT];
+    const auto value = [&](int k) { return D == 64 ? wv >= 2 : k >= LPT / 2; };
+    const auto second = [&](int k) { return (D == 64 ? wv & 1 : D == 128 ? wv >> 1 : k & 1) != 0; };
+    const auto load = [&](int st, int2 blocks) {
+        const int2 t = sub_tiles(see, see.at(min(st, last_stage)));
+#pragma unroll
+        for (int k = 0; k < LPT; ++k) {
+            // (an entry that names no block of the pool reads the last one: the rows are meaningless)
+            const size_t block = (size_t)min((unsigned)(second(k) ? blocks.y : blocks.x), (unsigned)a.num_blocks - 1) * stride;
+            const size_t off = block + (size_t)(((second(k) ? t.y : t.x) & (a.block_size - 1)) >> 4) * (16 * D);
+            const float2 s = __builtin_bit_cast(float2, *(scales_ptr)(uintptr_t)(sp + block));
+            scale_of[k] = value(k) ? s.y : s.x;
+            raw[k] = *reinterpret_cast<const uint4 *>((value(k) ? vp : kp) + off + ((kThreads * k + tid) & (D - 1)) * 16);
+        }
+    };
+    // Converts them to operands.  Values behind the tile's last position, which the cache may hold anything at, and those of a sub-tile that no token sees,
+    // become zeros.
+    const auto put = [&](int st, int buf) {
+        char *to = lds + buf * STAGE;
+        const int t0 = see.at(st);
+        const int2 from = sub_tiles(see, t0);
+        const bool part = (t0 + 32 > see.end) | (from.x == from.y);   // uniform
+        uint32_t bad = 0;
+#pragma unroll
+        for (int k = 0; k < LPT; ++k) {
+            const int sub = second(k) ? 1 : 0, u = (kThreads * k + tid) & (D - 1);
+            uint32_t y[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+            const float s = scale_of[k];
+            if (!value(k)) {
+                uint4 *p = reinterpret_cast<uint4 *>(to + sub * SUBK + ((u >> 4) * 32 + (u & 15)) * 16);
+                p[0] = make_uint4(from_codes<false>(y[0], s), from_codes<true>(y[0], s), from_codes<false>(y[1], s), from_codes<true>(y[1], s));
+                p[16] = make_uint4(from_codes<false>(y[2], s), from_codes<true>(y[2], s), from_codes<false>(y[3], s), from_codes<true>(y[3], s));
+            } else {
+                if (part) {
+                    const int left = (sub ? from.y == t0 : from.x != t0) ? 0 : see.end - (t0 + 16 * sub + (u >> 4 & 3) * 4);   // of the unit's four positions
+                    const uint32_t keep = left >= 4 ? 0xFFFFFFFFu : left <= 0 ? 0u : ~(0xFFFFFFFFu << (8 * left));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] &= keep;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    bad |= any_nan(y[e]) ? 1u : 0u;
+                    *reinterpret_cast<uint2 *>(to + VOFF + ((((u >> 6) * 4 + e) * 4 + (u >> 4 & 3)) * 16 + (u & 15)) * 16 + sub * 8) =
+                        make_uint2(from_codes<false>(y[e], s), from_codes<true>(y[e], s));
+                }
+            }
+        }
+        const bool any = __any(bad != 0);
+        if (lane == 0) wild_at[buf][wv] = any;
+    };
+
+    int2 next = make_int2(0, 0);
+    if (st0 < st1) {
+        const int2 now = lookup(st0);
+        next = lookup(st0 + 1);
+        load(st0, now);
+    }
+
+    // this lane's column in each block: (token, head), its position, its queries (of a negative scale: their negatives)
+    int pos[kCB];
+    size_t orow[kCB];
+    bf16x8 qb[kCB][NK];
+    const float scale = fabsf(a.scale_log2e);
+    const uint32_t flip = a.scale_log2e < 0.0f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int b = 0; b < kCB; ++b) {
+        const int col = b * 16 + j, tl = col / G, hd = col - tl * G, tok = wave_tok + tl;
+        const bool ok = col < TW * G && tok < n_new;
+        pos[b] = ok ? base_pos + tok : -1;
+        orow[b] = ((size_t)(first + (ok ? tok : 0)) * a.num_q_heads + g * G + hd) * D;
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            uint4 t = make_uint4(0, 0, 0, 0);
+            if (ok) t = *reinterpret_cast<const uint4 *>(static_cast<const char *>(a.q) + (orow[b] + 32 * i + 8 * qd) * 2);
+            t.x ^= flip; t.y ^= flip; t.z ^= flip; t.w ^= flip;
+            qb[b][i] = __builtin_bit_cast(bf16x8, t);
+        }
+    }
+    float m[kCB];
+    f32x4 o[kCB][NS], l[kCB];
+#pragma unroll
+    for (int b = 0; b < kCB; ++b) {
+        m[b] = kLeast;
+        l[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < NS; ++s) o[b][s] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const bf16x8 ones = __builtin_bit_cast(bf16x8, make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u));
+
+    f32x4 sc0[kCB], sc1[kCB];                            // scores: positions t + 4 qd + e and t + 16 + 4 qd + e of the lane's column
+    bf16x8 pw[kCB];
+    // Position p sees t + 4 qd + e: e <= lim and (e > lim - window or e < sinks - t - 4 qd), lim = p - t - 4 qd.
+    const auto visible = [&](int p, int t, int e) {
+        const int lim = p - t - 4 * qd;
+        return (e <= lim) & ((e > lim - w.window) | (e < w.sinks - t - 4 * qd));
+    };
+    const auto softmax = [&](int t0, bool masked) {
+        if (masked) {
+#pragma unroll
+            for (int b = 0; b < kCB; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (!visible(pos[b], t0, e)) sc0[b][e] = -INFINITY;
+                    if (!visible(pos[b], t0 + 16, e)) sc1[b][e] = -INFINITY;
+                }
+        }
+#pragma unroll
+        for (int b = 0; b < kCB; ++b) {
+            float sc[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sc[e] = e < 4 ? sc0[b][e] : sc1[b][e - 4];
+            float mx = sc[0];                            // (the median with infinity: the maximum)
+#pragma unroll
+            for (int e = 1; e < 8; ++e) mx = __builtin_amdgcn_fmed3f(mx, sc[e], INFINITY);
+            mx *= scale;
+            if (__any(mx - m[b] > kSlack)) {             // wave-uniform, rare after the first stages
+                mx = fmaxf(mx, __shfl_xor(mx, 16));
+                mx = fmaxf(mx, __shfl_xor(mx, 32));
+                const float mn = mx - m[b] > kSlack ? mx : m[b];
+                const float f = fast_exp2(m[b] - mn);
+                m[b] = mn;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) l[b][e] *= f;
+#pragma unroll
+                for (int s = 0; s < NS; ++s)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[b][s][e] *= f;
+            }
+            const float mn = m[b];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) pw[b][e] = (__bf16)fast_exp2(fmaf(sc[e], scale, -mn));
+        }
+    };
+
+    if (st0 < st1) {
+        put(st0, 0);
+        load(st0 + 1, next);
+        next = lookup(st0 + 2);
+    }
+    for (int st = st0; st < st1; ++st) {
+        const int cur = (st - st0) & 1;
+        const char *buf = lds + cur * STAGE;
+        __syncthreads();                                 // this stage is there, and the other buffer is read
+        if (st + 1 < st1) {
+            put(st + 1, cur ^ 1);
+            load(st + 2, next);
+            next = lookup(st + 3);
+        }
+        const int t0 = see.at(st);
+        const bool live = (t0 <= wave_max) & ((t0 + 31 >= wave_lo) | (t0 < w.sinks));   // uniform over the wave, as what follows
+        if (!live) continue;
+#pragma unroll
+        for (int b = 0; b < kCB; ++b) sc0[b] = sc1[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            const bf16x8 ka = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(buf + ((4 * i + qd) * 16 + j) * 16));
+            const bf16x8 kb = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(buf + SUBK + ((4 * i + qd) * 16 + j) * 16));
+#pragma unroll
+            for (int b = 0; b < kCB; ++b) {
+                sc0[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qb[b][i], sc0[b], 0, 0, 0);
+                sc1[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, qb[b][i], sc1[b], 0, 0, 0);
+            }
+        }
+        // (they are there before the way parts: see window_attn.hip)
+        if constexpr (kCB == 1) asm volatile("s_nop 7" : "+v"(sc0[0]), "+v"(sc1[0]));
+        else asm volatile("s_nop 7" : "+v"(sc0[0]), "+v"(sc1[0]), "+v"(sc0[1]), "+v"(sc1[1]));
+        const auto values = [&](int s) { return *reinterpret_cast<const uint4 *>(buf + VOFF + ((s * 4 + qd) * 16 + j) * 16); };
+        uint4 early[kEarly ? NS : 1];
+        if constexpr (kEarly) {
+#pragma unroll
+            for (int s = 0; s < NS; ++s) early[s] = values(s);
+        }
+        const auto vop = [&](int s) { return kEarly ? early[kEarly ? s : 0] : values(s); };
+        const bool masked = !((t0 + 31 <= wave_min) & ((t0 >= wave_hi) | (t0 + 32 <= w.sinks)));
+        softmax(t0, masked);
+#pragma unroll
+        for (int b = 0; b < kCB; ++b) l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pw[b], l[b], 0, 0, 0);
+        // A value that is NaN must not reach the columns that do not see it, and a zero weight does not silence it: where a stage that is seen in part has one,
+        // the products are taken without, and those of (is NaN) by (is seen) tell which outputs it makes NaN.
+        const bool apart = masked && (wild_at[cur][0] | wild_at[cur][1] | wild_at[cur][2] | wild_at[cur][3]) != 0;
+        if (__builtin_amdgcn_readfirstlane(apart)) {
+            bf16x8 seen[kCB];
+#pragma unroll
+            for (int b = 0; b < kCB; ++b) {
+                uint32_t x[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int t = k < 2 ? t0 : t0 + 16;
+                    x[k] = (visible(pos[b], t, 2 * (k & 1)) ? 0x3F80u : 0u) | (visible(pos[b], t, 2 * (k & 1) + 1) ? 0x3F800000u : 0u);
+                }
+                seen[b] = operand(x[0], x[1], x[2], x[3]);
+            }
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const uint4 v = vop(s);
+                uint32_t x[4] = {v.x, v.y, v.z, v.w}, is[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t nan = ((((x[k] & 0x7FFF7FFFu) + 0x007F007Fu) & 0x80008000u) >> 15) * 0xFFFFu;
+                    x[k] &= ~nan;
+                    is[k] = nan & 0x3F803F80u;
+                }
+#pragma unroll
+                for (int b = 0; b < kCB; ++b) {
+                    const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(is[0], is[1], is[2], is[3]), seen[b], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                    o[b][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(x[0], x[1], x[2], x[3]), pw[b], o[b][s], 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[b][s][e] = hit[e] > 0.0f ? __uint_as_float(0x7FC00000u) : o[b][s][e];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const bf16x8 v = __builtin_bit_cast(bf16x8, vop(s));
+#pragma unroll
+                for (int b = 0; b < kCB; ++b) o[b][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pw[b], o[b][s], 0, 0, 0);
+            }
+        }
+    }
+    // (the last products are there before what adds them up or stores them: see window_tiles.h)
+    asm volatile("s_nop 7" ::: "memory");
+#pragma unroll
+    for (int b = 0; b < kCB; ++b) asm volatile("" : "+v"(l[b]), "+v"(o[b][NS - 1]));
+
+    if (runs == 1) {
+#pragma unroll
+        for (int b = 0; b < kCB; ++b) store_column<NS>(static_cast<uint16_t *>(a.out) + orow[b], qd, pos[b] >= 0, 1.0f / l[b][0], o[b]);
+        return;
+    }
+    // the columns of each block as the wave holds them, and their (reference, sum); the last part to arrive adds them up
+    constexpr int kAll = kWaves * kCols;
+    constexpr size_t state = tile_state(D, kAll);
+    const size_t item = (size_t)at.item * a.num_kv_heads + g, step = (size_t)a.num_kv_heads * state;
+    float *first_part = a.partials + item * state, *to = first_part + at.at * step;
+    uint64_t *flags = reinterpret_cast<uint64_t *>(a.partials + (size_t)c.items * state) + item;
+    if (!none) {
+#pragma unroll
+        for (int b = 0; b < kCB; ++b) {
+            const int block = wv * kCB + b;
+#pragma unroll
+            for (int s = 0; s < 2 * NS; ++s)
+                put_shared(to + block * 16 * D + s * 128 + 2 * lane, o[b][s >> 1][2 * (s & 1)], o[b][s >> 1][2 * (s & 1) + 1]);
+            if (qd == 0) put_shared(to + kAll * D + 2 * (block * 16 + j), m[b], l[b][0]);
+        }
+    }
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();                                     // the workgroup's stores have arrived, and its LDS is free
+    int *is_last = reinterpret_cast<int *>(lds);
+    if (wv == 0) {
+        const bool all = report_run<true>(flags, a.num_kv_heads, at.at, runs, w.tag);
+        if (lane == 0) *is_last = all;
+    }
+    __syncthreads();
+    if (!*is_last || none) return;
+    // the parts in order, whichever workgroup this is: bit-reproducible
+#pragma unroll 1
+    for (int b = 0; b < kCB; ++b) {
+        const int block = wv * kCB + b;
+        float M = kLeast, L = 0.0f;
+        f32x4 A[NS];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) A[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+        for (int k = 0; k < runs; ++k) {
+            const float *from = first_part + k * step;
+            const float2 ml = get_shared(from + kAll * D + 2 * (block * 16 + j));
+            float2 x[2 * NS];
+#pragma unroll
+            for (int s = 0; s < 2 * NS; ++s) x[s] = get_shared(from + block * 16 * D + s * 128 + 2 * lane);
+            const float Mn = fmaxf(M, ml.x), f0 = fast_exp2(M - Mn), f = fast_exp2(ml.x - Mn);
+            L = L * f0 + ml.y * f;
+#pragma unroll
+            for (int s = 0; s < 2 * NS; ++s) {
+                A[s >> 1][2 * (s & 1)] = A[s >> 1][2 * (s & 1)] * f0 + x[s].x * f;
+                A[s >> 1][2 * (s & 1) + 1] = A[s >> 1][2 * (s & 1) + 1] * f0 + x[s].y * f;
+            }
+            M = Mn;
+        }
+        const int col = b * 16 + j, tl = col / G, tok = wave_tok + tl;
+        const bool ok = col < TW * G && tok < n_new;
+        store_column<NS>(static_cast<uint16_t *>(a.out) + ((size_t)(first + (ok ? tok : 0)) * a.num_q_heads + g * G + (ok ? col - tl * G : 0)) * D, qd, ok, 1.0f / L, A);
+    }
+}
+
+// A wavefront per token and kv head (or pass), weights as pairs of bf16: for more than 32 heads to a kv head, and where a caller asks for it.
+template <int D>
+__global__ __launch_bounds__(kThreads, D >= 256 ? 1 : 2) void kv8_rows(const WindowArgs w)
+{
+    const DecodeArgs &a = w.d;
+    const int GH = a.heads_per_pass, HC = a.num_kv_heads * a.passes;
+    const long long item = (long long)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (item >= (long long)w.total_tokens * HC) return;
+    const int n = (int)(item / HC), hc = (int)(item - (long long)n * HC), h0 = hc * GH;
+    const auto [r, first, count, ctx] = new_tokens_at(w.q_start, a.ctx_lens, a.batch, n, [](int q, int) { return q; });
+    // (a context shorter than its new tokens, or longer than the table row: nothing is read or written)
+    if (n < first || n >= first + count || ctx < count || ctx > a.max_blocks * a.block_size) return;
+    const Sight<32> see(__builtin_amdgcn_readfirstlane(ctx - count + (n - first) + 1), w.window, w.sinks);
+    uint16_t *out = static_cast<uint16_t *>(a.out) + ((size_t)n * a.num_q_heads + h0) * D;
+    CodesReducer<D>::run(a, __builtin_amdgcn_readfirstlane(r), (size_t)n, hc / a.passes, h0, GH, see, 0, see.units, [&](int h, int d, float, float L, const auto &A) {
+        const float inv = 1.0f / L;
+        *reinterpret_cast<uint2 *>(out + h * D + d) = make_uint2(pack_bf16(A[0] * inv, A[1] * inv), pack_bf16(A[2] * inv, A[3] * inv));
+    });
+}
+
+template <int D, int kCB>
+hipError_t launch_tiles(const WindowArgs &w, hipStream_t s)
+{
+    const DecodeArgs &a = w.d;
+    const int WT = kWaves * (16 * kCB / (a.num_q_heads / a.num_kv_heads));
+    const long long tiles = (long long)w.total_tokens / WT + a.batch, heads = a.num_kv_heads;
+    Tiling c = {0, 0};
+    if (a.batch <= kMostRequests) {
+        // Parts are no more than 5 / 3 of the places (see kv8_decode.hip); two workgroups fit a CU.
+        const long long state = (long long)tile_state(D, kWaves * 16 * kCB) * (long long)sizeof(float), room = (long long)a.partial_capacity / (state + 8);
+        c.places = (int)std::min(512LL, room * 3 / 5 - 1);
+        if (c.places < 1) c.places = 0;
+        c.items = (int)std::min(room, 1024LL);
+    }
+    const long long grid = (tiles * heads + (c.places > 0 ? 2LL * c.places : 0) + heads - 1) / heads * heads;
+    if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((kv8_tiles<D, kCB>), dim3((unsigned)grid), dim3(kThreads), 0, s, w, c);
+    return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch(const WindowArgs &w, hipStream_t s)
+{
+    const DecodeArgs &a = w.d;
+    const int G = a.num_q_heads / a.num_kv_heads;
+    if (G > 32 || w.force_rows) {
+        const long long items = (long long)w.total_tokens * a.num_kv_heads * a.passes;
+        if (items > 0x7fffffffLL * kWaves) return hipErrorInvalidValue;
+        hipLaunchKernelGGL(kv8_rows<D>, dim3((unsigned)((items + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, w);
+        return hipGetLastError();
+    }
+    const bool narrow = G <= 16 && (long long)w.max_new_tokens * G <= 256;
+    return narrow ? launch_tiles<D, 1>(w, s) : launch_tiles<D, 2>(w, s);
+}
+
+}  // namespace
+
+hipError_t launch_kv8_prefill(const WindowArgs &w, hipStream_t stream)
+{
+    if (w.d.batch == 0 || w.total_tokens == 0) return hipSuccess;
+    if (w.d.head_dim == 64) return launch<64>(w, stream);
+    if (w.d.head_dim == 128) return launch<128>(w, stream);
+    if (w.d.head_dim == 256) return launch<256>(w, stream);
+    return hipErrorInvalidValue;
+}
+
+}  // namespace lamps
