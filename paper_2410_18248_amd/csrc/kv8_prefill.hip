@@ -126,20 +126,21 @@ __device__ __forceinline__ bool find_whole_tile(const WindowArgs &w, int WT, int
 
 constexpr size_t tile_state(int D, int columns) { return (size_t)columns * (D + 2); }   // floats
 
-template <int D, int kCB>
+template <int D, int kCB, bool WINDOW>
 __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_tiles(const WindowArgs w, const Tiling c)
 {
-    constexpr int kCols = 16 * kCB, NK = D / 32, NS = D / 16, LPT = D / 64;
+    constexpr int kCols = 16 * kCB, NK = D / 32, NS = D / 16;
     constexpr int SUBK = 16 * D * 2, VOFF = 2 * SUBK, STAGE = 4 * SUBK;   // bytes of a sub-tile of keys, where values begin, of a stage
-    constexpr bool kEarly = D <= 64 || (D == 128 && kCB == 1);   // values are asked for in front of the softmax: where registers hold them
+    constexpr bool kHold = D <= 128;                     // operands of a stage are held in registers
     __shared__ __align__(16) char lds[2 * STAGE];
-    __shared__ uint32_t wild_at[2][kWaves];
+    constexpr int SUBS = D == 256 ? 2 : 1, KINDS = D == 64 ? 1 : 2;   // of a thread's units: sub-tiles, keys and values
+    __shared__ uint32_t wild_at[2][kWaves * SUBS];
 
     const DecodeArgs &a = w.d;
     const int G = a.num_q_heads / a.num_kv_heads, TW = kCols / G, WT = kWaves * TW;
     TilePiece at;
     // (heads next to each other: with 8 of them and more all tiles of one go to one XCD, whose L2 has its keys and values)
-    const int piece = (int)((unsigned)blockIdx.x / (unsigned)a.num_kv_heads);
+    const int piece = __builtin_amdgcn_readfirstlane((int)((unsigned)blockIdx.x / (unsigned)a.num_kv_heads));
     at.g = blockIdx.x - piece * a.num_kv_heads;
     if (c.places == 0 ? !find_whole_tile(w, WT, piece, at) : a.batch <= 64 ? !find_tile<1>(w, c, WT, piece, at) : !find_tile<4>(w, c, WT, piece, at)) return;
     const int g = at.g, first = at.first, base_pos = at.ctx - at.n_new, n_new = min(at.n_new, w.total_tokens - first);
@@ -147,7 +148,8 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
 
     // what the tile walks over, and the part of it that is this workgroup's
     const int p_first = base_pos + at.tile * WT, p_last = base_pos + min(n_new, (at.tile + 1) * WT) - 1;
-    const Sight<32> see(p_last + 1, max(0, p_first - w.window + 1), w.sinks, std::true_type{});
+    const Sight<32> see = WINDOW ? Sight<32>(p_last + 1, max(0, p_first - w.window + 1), w.sinks, std::true_type{}) : Sight<32>(p_last + 1, 0, 0, std::true_type{});
+    const auto position = [&](int st) { return WINDOW ? see.at(st) : st * 32; };
     int st0 = 0, st1 = see.units, runs = 1;
     if (at.runs > 1) {
         // (a tile of earlier tokens may have less than the request's last one, by which the parts are counted)
@@ -157,6 +159,8 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
         st0 = at.at * each;
         st1 = min(see.units, st0 + each);
     }
+    st0 = __builtin_amdgcn_readfirstlane(st0);
+    st1 = __builtin_amdgcn_readfirstlane(st1);
     // the wave's own tokens; none: positions that see nothing
     const int wave_tok = at.tile * WT + wv * TW;
     const bool none = wave_tok >= n_new;
@@ -164,74 +168,108 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
     const int wave_max = __builtin_amdgcn_readfirstlane(none ? -1 : base_pos + min(n_new, wave_tok + TW) - 1);
     const int wave_hi = wave_max - w.window + 1, wave_lo = wave_min - w.window + 1;   // where the windows of the wave's last and first token begin
 
+    // Thread's units of a stage, 16 bytes of codes.  Heads of 128: a wave half of a sub-tile's keys and the same of its values; of 64: its keys or its values; of
+    // 256: a quarter of both sub-tiles' of both.
+    const int wave_sub = D == 64 ? wv & 1 : D == 128 ? wv >> 1 : 0, wave_kind = D == 64 ? wv >> 1 : 0;
+    const int u = D == 64 ? lane : D == 128 ? (wv & 1) * 64 + lane : tid;   // of the sub-tile
     const table_ptr table = (table_ptr)(uintptr_t)(a.block_table + (size_t)at.r * a.max_blocks);
-    const size_t tile_bytes = (size_t)a.block_size * D, slice = codes_slice(a.num_kv_heads, a.block_size, D), stride = a.num_layers * slice;
-    const char *k0 = static_cast<const char *>(a.k_pool) + a.layer * slice;
-    const char *kp = k0 + g * tile_bytes, *vp = static_cast<const char *>(a.v_pool) + a.layer * slice + g * tile_bytes;
-    const char *sp = k0 + a.num_kv_heads * tile_bytes + g * 8;
-    const int last_pos = a.max_blocks * a.block_size - 1, last_stage = see.units - 1;
-    const auto lookup = [&](int st) {
-        const int2 t = sub_tiles(see, see.at(min(st, last_stage)));
-        return make_int2(table[t.x >> a.log2_block_size], table[t.y >> a.log2_block_size]);
+    const uint32_t tile_bytes = (uint32_t)a.block_size * D, slice = (uint32_t)codes_slice(a.num_kv_heads, a.block_size, D), stride = a.num_layers * slice;   // (the launcher has checked that it fits)
+    const char *k0 = static_cast<const char *>(a.k_pool) + (size_t)a.layer * slice;
+    const char *kp = k0 + (size_t)g * tile_bytes, *vp = static_cast<const char *>(a.v_pool) + (size_t)a.layer * slice + (size_t)g * tile_bytes;
+    const char *sp = k0 + (size_t)a.num_kv_heads * tile_bytes + g * 8;
+    const uint32_t last_block = (uint32_t)a.num_blocks - 1, u16 = u * 16;
+    const int last_stage = see.units - 1, in_block = (a.block_size - 1) & ~15;
+    struct Places {
+        uint32_t block[SUBS], at[SUBS];                  // where a sub-tile is: a block, and where in its tile
     };
-    // This thread's units of a stage, 16 bytes of codes: units of keys of both sub-tiles, then of values.  All of a wave's are of one kind and sub-tile.
-    uint4 raw[LPT];
-    float scale_of[LPT];
-    const auto value = [&](int k) { return D == 64 ? wv >= 2 : k >= LPT / 2; };
-    const auto second = [&](int k) { return (D == 64 ? wv & 1 : D == 128 ? wv >> 1 : k & 1) != 0; };
-    const auto load = [&](int st, int2 blocks) {
-        const int2 t = sub_tiles(see, see.at(min(st, last_stage)));
+    const auto lookup = [&](int st) {
+        const int t = position(min(st, last_stage));
+        Places x;
 #pragma unroll
-        for (int k = 0; k < LPT; ++k) {
+        for (int i = 0; i < SUBS; ++i) {
+            const int sub = SUBS == 2 ? i : wave_sub;
+            int p;
+            if constexpr (WINDOW) {
+                const int2 both = sub_tiles(see, t);
+                p = sub ? both.y : both.x;
+            } else {
+                p = t + 16 * sub < see.end ? t + 16 * sub : t;
+            }
             // (an entry that names no block of the pool reads the last one: the rows are meaningless)
-            const size_t block = (size_t)min((unsigned)(second(k) ? blocks.y : blocks.x), (unsigned)a.num_blocks - 1) * stride;
-            const size_t off = block + (size_t)(((second(k) ? t.y : t.x) & (a.block_size - 1)) >> 4) * (16 * D);
-            const float2 s = __builtin_bit_cast(float2, *(scales_ptr)(uintptr_t)(sp + block));
-            scale_of[k] = value(k) ? s.y : s.x;
-            raw[k] = *reinterpret_cast<const uint4 *>((value(k) ? vp : kp) + off + ((kThreads * k + tid) & (D - 1)) * 16);
+            x.block[i] = min((uint32_t)table[p >> a.log2_block_size], last_block);
+            x.at[i] = (uint32_t)(p & in_block) * D;
+        }
+        return x;
+    };
+    uint4 raw[SUBS][KINDS];
+    float2 scale_of[SUBS];
+    const auto load = [&](const Places &x) {
+#pragma unroll
+        for (int i = 0; i < SUBS; ++i) {
+            const uint64_t block = (uint64_t)x.block[i] * stride, off = block + x.at[i];
+            scale_of[i] = __builtin_bit_cast(float2, *(scales_ptr)(uintptr_t)(sp + block));
+            if constexpr (KINDS == 2) {
+                raw[i][0] = *reinterpret_cast<const uint4 *>(kp + off + u16);
+                raw[i][1] = *reinterpret_cast<const uint4 *>(vp + off + u16);
+            } else {
+                raw[i][0] = *reinterpret_cast<const uint4 *>((wave_kind ? vp : kp) + off + u16);
+            }
         }
     };
     // Converts them to operands.  Values behind the tile's last position, which the cache may hold anything at, and those of a sub-tile that no token sees,
-    // become zeros.
+    // become zeros; whether one that is left is NaN matters where a stage is not seen by all.
+    const int wg_min = p_first, wg_hi = p_last - w.window + 1;
+    const uint32_t key_to = (u >> 4) * 512 + (u & 15) * 16, value_to = VOFF + ((u >> 6) * 256 + (u >> 4 & 3) * 16 + (u & 15)) * 16;
     const auto put = [&](int st, int buf) {
         char *to = lds + buf * STAGE;
-        const int t0 = see.at(st);
-        const int2 from = sub_tiles(see, t0);
-        const bool part = (t0 + 32 > see.end) | (from.x == from.y);   // uniform
-        uint32_t bad = 0;
+        const int t0 = position(min(st, last_stage));
+        const bool edge = (t0 + 31 > wg_min) | (WINDOW && t0 < wg_hi);
 #pragma unroll
-        for (int k = 0; k < LPT; ++k) {
-            const int sub = second(k) ? 1 : 0, u = (kThreads * k + tid) & (D - 1);
-            uint32_t y[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
-            const float s = scale_of[k];
-            if (!value(k)) {
-                uint4 *p = reinterpret_cast<uint4 *>(to + sub * SUBK + ((u >> 4) * 32 + (u & 15)) * 16);
-                p[0] = make_uint4(from_codes<false>(y[0], s), from_codes<true>(y[0], s), from_codes<false>(y[1], s), from_codes<true>(y[1], s));
-                p[16] = make_uint4(from_codes<false>(y[2], s), from_codes<true>(y[2], s), from_codes<false>(y[3], s), from_codes<true>(y[3], s));
-            } else {
-                if (part) {
-                    const int left = (sub ? from.y == t0 : from.x != t0) ? 0 : see.end - (t0 + 16 * sub + (u >> 4 & 3) * 4);   // of the unit's four positions
-                    const uint32_t keep = left >= 4 ? 0xFFFFFFFFu : left <= 0 ? 0u : ~(0xFFFFFFFFu << (8 * left));
+        for (int i = 0; i < SUBS; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) y[e] &= keep;
-                }
+            for (int k = 0; k < KINDS; ++k) {
+                const int sub = SUBS == 2 ? i : wave_sub;
+                const uint4 y = raw[i][k];
+                if (KINDS == 2 ? k == 0 : wave_kind == 0) {
+                    const float s = scale_of[i].x;
+                    uint4 *p = reinterpret_cast<uint4 *>(to + sub * SUBK + key_to);
+                    p[0] = make_uint4(from_codes<false>(y.x, s), from_codes<true>(y.x, s), from_codes<false>(y.y, s), from_codes<true>(y.y, s));
+                    p[16] = make_uint4(from_codes<false>(y.z, s), from_codes<true>(y.z, s), from_codes<false>(y.w, s), from_codes<true>(y.w, s));
+                } else {
+                    const float s = scale_of[i].y;
+                    uint32_t x[4] = {y.x, y.y, y.z, y.w};
+                    if (edge) {                          // uniform
+                        int left = see.end - (t0 + 16 * sub + (u >> 4 & 3) * 4);   // of the unit's four positions
+                        if constexpr (WINDOW) {
+                            const int2 both = sub_tiles(see, t0);
+                            if ((sub ? both.y : both.x) != t0 + 16 * sub) left = 0;
+                        }
+                        const uint32_t keep = left >= 4 ? 0xFFFFFFFFu : left <= 0 ? 0u : ~(0xFFFFFFFFu << (8 * left));
+                        bool bad = false;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    bad |= any_nan(y[e]) ? 1u : 0u;
-                    *reinterpret_cast<uint2 *>(to + VOFF + ((((u >> 6) * 4 + e) * 4 + (u >> 4 & 3)) * 16 + (u & 15)) * 16 + sub * 8) =
-                        make_uint2(from_codes<false>(y[e], s), from_codes<true>(y[e], s));
+                        for (int e = 0; e < 4; ++e) {
+                            x[e] &= keep;
+                            bad |= any_nan(x[e]);
+                        }
+                        const bool any = __any(bad);
+                        if (lane == 0) wild_at[buf][kWaves * i + wv] = any;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        *reinterpret_cast<uint2 *>(to + value_to + e * 1024 + sub * 8) = make_uint2(from_codes<false>(x[e], s), from_codes<true>(x[e], s));
                 }
             }
-        }
-        const bool any = __any(bad != 0);
-        if (lane == 0) wild_at[buf][wv] = any;
     };
 
-    int2 next = make_int2(0, 0);
+    if (lane == 0) {
+#pragma unroll
+        for (int i = 0; i < SUBS; ++i) wild_at[0][kWaves * i + wv] = wild_at[1][kWaves * i + wv] = 0;
+    }
+    Places next = {};
     if (st0 < st1) {
-        const int2 now = lookup(st0);
+        const Places now = lookup(st0);
         next = lookup(st0 + 1);
-        load(st0, now);
+        load(now);
     }
 
     // this lane's column in each block: (token, head), its position, its queries (of a negative scale: their negatives)
@@ -270,7 +308,28 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
     // Position p sees t + 4 qd + e: e <= lim and (e > lim - window or e < sinks - t - 4 qd), lim = p - t - 4 qd.
     const auto visible = [&](int p, int t, int e) {
         const int lim = p - t - 4 * qd;
-        return (e <= lim) & ((e > lim - w.window) | (e < w.sinks - t - 4 * qd));
+        return WINDOW ? (e <= lim) & ((e > lim - w.window) | (e < w.sinks - t - 4 * qd)) : e <= lim;
+    };
+    // The weights of block b, by the reference that it has; the largest of them, found by packed maxima of pairs: they are not negative, so their bits compare as
+    // they do, and as those of fp16 numbers.  One of 2^kSlack and more, or no finite one, asks for another reference: rare after the first stages.
+    typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+    const auto weigh = [&](int b) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            pw[b][e] = (__bf16)fast_exp2(fmaf(sc0[b][e], scale, -m[b]));
+            pw[b][4 + e] = (__bf16)fast_exp2(fmaf(sc1[b][e], scale, -m[b]));
+        }
+        uint4 y = __builtin_bit_cast(uint4, pw[b]);
+        asm("" : "+v"(y.x), "+v"(y.y), "+v"(y.z), "+v"(y.w));   // (pairs from here on: carried over the branch one by one, they are converted twice)
+        pw[b] = __builtin_bit_cast(bf16x8, y);
+        uint32_t most;
+        asm("v_pk_maximum3_f16 %0, %1, %2, %3" : "=v"(most) : "v"(y.x), "v"(y.y), "v"(y.z));
+        asm("v_pk_maximum3_f16 %0, %1, %2, %2" : "=v"(most) : "v"(most), "v"(y.w));
+        return most;
+    };
+    const auto over = [](uint32_t most) {
+        constexpr unsigned short kBelow = ((127 + (int)kSlack) << 7) - 1;   // the bf16 in front of 2^kSlack
+        return __any(__builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, most), u16x2{kBelow, kBelow})) != 0);
     };
     const auto softmax = [&](int t0, bool masked) {
         if (masked) {
@@ -282,20 +341,23 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
                     if (!visible(pos[b], t0 + 16, e)) sc1[b][e] = -INFINITY;
                 }
         }
+        uint32_t most[kCB], all = 0;
 #pragma unroll
         for (int b = 0; b < kCB; ++b) {
-            float sc[8];
+            most[b] = weigh(b);
+            if (b == 0) all = most[0];
+            else asm("v_pk_maximum3_f16 %0, %1, %2, %2" : "=v"(all) : "v"(all), "v"(most[b]));
+        }
+        if (over(all)) {                                 // wave-uniform
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sc[e] = e < 4 ? sc0[b][e] : sc1[b][e - 4];
-            float mx = sc[0];                            // (the median with infinity: the maximum)
+            for (int b = 0; b < kCB; ++b) {
+                if (kCB > 1 && !over(most[b])) continue;
+                float mx = sc0[b][0];                    // (the median with infinity: the maximum)
 #pragma unroll
-            for (int e = 1; e < 8; ++e) mx = __builtin_amdgcn_fmed3f(mx, sc[e], INFINITY);
-            mx *= scale;
-            if (__any(mx - m[b] > kSlack)) {             // wave-uniform, rare after the first stages
+                for (int e = 1; e < 8; ++e) mx = __builtin_amdgcn_fmed3f(mx, e < 4 ? sc0[b][e & 3] : sc1[b][e & 3], INFINITY);
                 mx = fmaxf(mx, __shfl_xor(mx, 16));
-                mx = fmaxf(mx, __shfl_xor(mx, 32));
-                const float mn = mx - m[b] > kSlack ? mx : m[b];
-                const float f = fast_exp2(m[b] - mn);
+                mx = fmaxf(mx, __shfl_xor(mx, 32)) * scale;
+                const float mn = mx - m[b] > kSlack ? mx : m[b], f = fast_exp2(m[b] - mn);
                 m[b] = mn;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) l[b][e] *= f;
@@ -303,97 +365,125 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
                 for (int s = 0; s < NS; ++s)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[b][s][e] *= f;
+                weigh(b);
             }
-            const float mn = m[b];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) pw[b][e] = (__bf16)fast_exp2(fmaf(sc[e], scale, -mn));
         }
     };
 
+    // A value that is NaN must not reach the columns that do not see it, and a zero weight does not silence it: where a stage that is seen in part has one,
+    // the products are taken without, and those of (is NaN) by (is seen) tell which outputs it makes NaN.
+    const auto set_apart = [&](int s, int t0, uint4 &v) {
+        uint32_t x[4] = {v.x, v.y, v.z, v.w}, is[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t nan = ((((x[k] & 0x7FFF7FFFu) + 0x007F007Fu) & 0x80008000u) >> 15) * 0xFFFFu;
+            x[k] &= ~nan;
+            is[k] = nan & 0x3F803F80u;
+        }
+        v = make_uint4(x[0], x[1], x[2], x[3]);
+#pragma unroll
+        for (int b = 0; b < kCB; ++b) {
+            uint32_t y[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int t = k < 2 ? t0 : t0 + 16;
+                y[k] = (visible(pos[b], t, 2 * (k & 1)) ? 0x3F80u : 0u) | (visible(pos[b], t, 2 * (k & 1) + 1) ? 0x3F800000u : 0u);
+            }
+            const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(is[0], is[1], is[2], is[3]), operand(y[0], y[1], y[2], y[3]), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[b][s][e] += hit[e] > 0.0f ? __uint_as_float(0x7FC00000u) : 0.0f;
+        }
+    };
+
+    // Operands of keys for the stage at hand are in registers where its iteration begins, those of values are asked for in front of its products
+    // (heads of 256: both where they are used, for want of registers).  Behind the softmax a barrier: everyone has what the stage's buffer held, and the other one is
+    // whole; the next keys are read, and the next stage but one is converted, while the matrix cores multiply values.
+    bf16x8 kop[kHold ? NK : 1][2];
+    uint4 vheld[kHold ? NS : 1];
+    const char *mine = lds + lane * 16;                  // (unit qd * 16 + j)
+    const auto key = [&](const char *buf, int i, int h) { return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(buf + h * SUBK + i * 1024)); };
+    const auto read_k = [&](const char *buf) {
+        if constexpr (kHold) {
+#pragma unroll
+            for (int i = 0; i < NK; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) kop[i][h] = key(buf, i, h);
+        }
+    };
     if (st0 < st1) {
         put(st0, 0);
-        load(st0 + 1, next);
+        load(next);
         next = lookup(st0 + 2);
+        put(st0 + 1, 1);                                 // (past the last stage: the last one once more, which nobody reads)
+        load(next);
+        next = lookup(st0 + 3);
     }
+    __syncthreads();
+    if (st0 < st1) read_k(mine);
     for (int st = st0; st < st1; ++st) {
         const int cur = (st - st0) & 1;
-        const char *buf = lds + cur * STAGE;
-        __syncthreads();                                 // this stage is there, and the other buffer is read
-        if (st + 1 < st1) {
-            put(st + 1, cur ^ 1);
-            load(st + 2, next);
-            next = lookup(st + 3);
-        }
-        const int t0 = see.at(st);
-        const bool live = (t0 <= wave_max) & ((t0 + 31 >= wave_lo) | (t0 < w.sinks));   // uniform over the wave, as what follows
-        if (!live) continue;
+        const char *buf = mine + cur * STAGE;
+        const int t0 = position(st);
+        const bool live = (t0 <= wave_max) & (!WINDOW | (t0 + 31 >= wave_lo) | (t0 < w.sinks));   // uniform over the wave, as what follows
+        const bool masked = !((t0 + 31 <= wave_min) & (!WINDOW | (t0 >= wave_hi) | (t0 + 32 <= w.sinks)));
+        const auto values = [&](int s) { return *reinterpret_cast<const uint4 *>(buf + VOFF + s * 1024); };
+        const auto vop = [&](int s) { return kHold ? vheld[kHold ? s : 0] : values(s); };
+        bool apart = false;
+        if (live) {
+            if constexpr (kHold) {
 #pragma unroll
-        for (int b = 0; b < kCB; ++b) sc0[b] = sc1[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < NK; ++i) {
-            const bf16x8 ka = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(buf + ((4 * i + qd) * 16 + j) * 16));
-            const bf16x8 kb = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(buf + SUBK + ((4 * i + qd) * 16 + j) * 16));
-#pragma unroll
-            for (int b = 0; b < kCB; ++b) {
-                sc0[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qb[b][i], sc0[b], 0, 0, 0);
-                sc1[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, qb[b][i], sc1[b], 0, 0, 0);
-            }
-        }
-        // (they are there before the way parts: see window_attn.hip)
-        if constexpr (kCB == 1) asm volatile("s_nop 7" : "+v"(sc0[0]), "+v"(sc1[0]));
-        else asm volatile("s_nop 7" : "+v"(sc0[0]), "+v"(sc1[0]), "+v"(sc0[1]), "+v"(sc1[1]));
-        const auto values = [&](int s) { return *reinterpret_cast<const uint4 *>(buf + VOFF + ((s * 4 + qd) * 16 + j) * 16); };
-        uint4 early[kEarly ? NS : 1];
-        if constexpr (kEarly) {
-#pragma unroll
-            for (int s = 0; s < NS; ++s) early[s] = values(s);
-        }
-        const auto vop = [&](int s) { return kEarly ? early[kEarly ? s : 0] : values(s); };
-        const bool masked = !((t0 + 31 <= wave_min) & ((t0 >= wave_hi) | (t0 + 32 <= w.sinks)));
-        softmax(t0, masked);
-#pragma unroll
-        for (int b = 0; b < kCB; ++b) l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pw[b], l[b], 0, 0, 0);
-        // A value that is NaN must not reach the columns that do not see it, and a zero weight does not silence it: where a stage that is seen in part has one,
-        // the products are taken without, and those of (is NaN) by (is seen) tell which outputs it makes NaN.
-        const bool apart = masked && (wild_at[cur][0] | wild_at[cur][1] | wild_at[cur][2] | wild_at[cur][3]) != 0;
-        if (__builtin_amdgcn_readfirstlane(apart)) {
-            bf16x8 seen[kCB];
-#pragma unroll
-            for (int b = 0; b < kCB; ++b) {
-                uint32_t x[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int t = k < 2 ? t0 : t0 + 16;
-                    x[k] = (visible(pos[b], t, 2 * (k & 1)) ? 0x3F80u : 0u) | (visible(pos[b], t, 2 * (k & 1) + 1) ? 0x3F800000u : 0u);
-                }
-                seen[b] = operand(x[0], x[1], x[2], x[3]);
+                for (int s = 0; s < NS; ++s) vheld[s] = values(s);
             }
 #pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                const uint4 v = vop(s);
-                uint32_t x[4] = {v.x, v.y, v.z, v.w}, is[4];
+            for (int b = 0; b < kCB; ++b) sc0[b] = sc1[b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t nan = ((((x[k] & 0x7FFF7FFFu) + 0x007F007Fu) & 0x80008000u) >> 15) * 0xFFFFu;
-                    x[k] &= ~nan;
-                    is[k] = nan & 0x3F803F80u;
-                }
+            for (int i = 0; i < NK; ++i) {
+                const bf16x8 ka = kHold ? kop[kHold ? i : 0][0] : key(buf, i, 0), kb = kHold ? kop[kHold ? i : 0][1] : key(buf, i, 1);
 #pragma unroll
                 for (int b = 0; b < kCB; ++b) {
-                    const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(is[0], is[1], is[2], is[3]), seen[b], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-                    o[b][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(x[0], x[1], x[2], x[3]), pw[b], o[b][s], 0, 0, 0);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[b][s][e] = hit[e] > 0.0f ? __uint_as_float(0x7FC00000u) : o[b][s][e];
+                    sc0[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qb[b][i], sc0[b], 0, 0, 0);
+                    sc1[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, qb[b][i], sc1[b], 0, 0, 0);
                 }
             }
-        } else {
+            // (they are there before the way parts: see window_attn.hip)
+            if constexpr (kCB == 1) asm volatile("s_nop 7" : "+v"(sc0[0]), "+v"(sc1[0]));
+            else asm volatile("s_nop 7" : "+v"(sc0[0]), "+v"(sc1[0]), "+v"(sc0[1]), "+v"(sc1[1]));
+            softmax(t0, masked);
+            if (masked) {
+                uint32_t any = 0;
 #pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                const bf16x8 v = __builtin_bit_cast(bf16x8, vop(s));
+                for (int k = 0; k < kWaves * SUBS; ++k) any |= wild_at[cur][k];
+                apart = __builtin_amdgcn_readfirstlane(any) != 0;
+            }
+            if constexpr (kHold) {
+                if (apart) {
 #pragma unroll
-                for (int b = 0; b < kCB; ++b) o[b][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pw[b], o[b][s], 0, 0, 0);
+                    for (int s = 0; s < NS; ++s) set_apart(s, t0, vheld[s]);
+                }
             }
         }
+        const auto turn = [&]() {
+            __syncthreads();
+            read_k(mine + (cur ^ 1) * STAGE);
+            put(st + 2, cur);
+            load(next);
+            next = lookup(st + 4);
+        };
+        if constexpr (kHold) turn();
+        if (!live) {
+            if constexpr (!kHold) turn();
+            continue;
+        }
+#pragma unroll
+        for (int b = 0; b < kCB; ++b) l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pw[b], l[b], 0, 0, 0);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            uint4 v = vop(s);
+            if (!kHold && apart) set_apart(s, t0, v);    // uniform
+#pragma unroll
+            for (int b = 0; b < kCB; ++b) o[b][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), pw[b], o[b][s], 0, 0, 0);
+        }
+        if constexpr (!kHold) turn();
     }
     // (the last products are there before what adds them up or stores them: see window_tiles.h)
     asm volatile("s_nop 7" ::: "memory");
@@ -496,7 +586,9 @@ hipError_t launch_tiles(const WindowArgs &w, hipStream_t s)
     }
     const long long grid = (tiles * heads + (c.places > 0 ? 2LL * c.places : 0) + heads - 1) / heads * heads;
     if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((kv8_tiles<D, kCB>), dim3((unsigned)grid), dim3(kThreads), 0, s, w, c);
+    const bool window = w.window < (long long)a.max_blocks * a.block_size;
+    if (window) hipLaunchKernelGGL((kv8_tiles<D, kCB, true>), dim3((unsigned)grid), dim3(kThreads), 0, s, w, c);
+    else hipLaunchKernelGGL((kv8_tiles<D, kCB, false>), dim3((unsigned)grid), dim3(kThreads), 0, s, w, c);
     return hipGetLastError();
 }
 
@@ -505,7 +597,9 @@ hipError_t launch(const WindowArgs &w, hipStream_t s)
 {
     const DecodeArgs &a = w.d;
     const int G = a.num_q_heads / a.num_kv_heads;
-    if (G > 32 || w.force_rows) {
+    // (the tiles' kernel keeps the distance between two blocks of a pool in 32 bits)
+    const bool far = a.num_layers * codes_slice(a.num_kv_heads, a.block_size, D) > 0xffffffffull;
+    if (G > 32 || w.force_rows || far) {
         const long long items = (long long)w.total_tokens * a.num_kv_heads * a.passes;
         if (items > 0x7fffffffLL * kWaves) return hipErrorInvalidValue;
         hipLaunchKernelGGL(kv8_rows<D>, dim3((unsigned)((items + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, w);
