@@ -414,14 +414,24 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
         put(st0, 0);
         load(next);
         next = lookup(st0 + 2);
-        put(st0 + 1, 1);                                 // (past the last stage: the last one once more, which nobody reads)
-        load(next);
-        next = lookup(st0 + 3);
+        if constexpr (kHold) {
+            put(st0 + 1, 1);                             // (past the last stage: the last one once more, which nobody reads)
+            load(next);
+            next = lookup(st0 + 3);
+        }
     }
-    __syncthreads();
-    if (st0 < st1) read_k(mine);
+    if constexpr (kHold) {
+        __syncthreads();
+        if (st0 < st1) read_k(mine);
+    }
     for (int st = st0; st < st1; ++st) {
         const int cur = (st - st0) & 1;
+        if constexpr (!kHold) {
+            __syncthreads();
+            put(st + 1, cur ^ 1);
+            load(next);
+            next = lookup(st + 3);
+        }
         const char *buf = mine + cur * STAGE;
         const int t0 = position(st);
         const bool live = (t0 <= wave_max) & (!WINDOW | (t0 + 31 >= wave_lo) | (t0 < w.sinks));   // uniform over the wave, as what follows
@@ -462,18 +472,14 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
                 }
             }
         }
-        const auto turn = [&]() {
+        if constexpr (kHold) {
             __syncthreads();
             read_k(mine + (cur ^ 1) * STAGE);
             put(st + 2, cur);
             load(next);
             next = lookup(st + 4);
-        };
-        if constexpr (kHold) turn();
-        if (!live) {
-            if constexpr (!kHold) turn();
-            continue;
         }
+        if (!live) continue;
 #pragma unroll
         for (int b = 0; b < kCB; ++b) l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pw[b], l[b], 0, 0, 0);
 #pragma unroll
@@ -483,7 +489,6 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
 #pragma unroll
             for (int b = 0; b < kCB; ++b) o[b][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), pw[b], o[b][s], 0, 0, 0);
         }
-        if constexpr (!kHold) turn();
     }
     // (the last products are there before what adds them up or stores them: see window_tiles.h)
     asm volatile("s_nop 7" ::: "memory");
