@@ -23,8 +23,9 @@ namespace lamps {
 namespace {
 
 struct Tiling {
-    int items;                                           // workgroups of a head
+    int items;                                           // parts that there is room for
     int places;                                          // workgroups that all work is dealt to evenly where requests are cut; 0: none is
+    int later;                                           // parts are added up by a second launch
 };
 constexpr int kMostRequests = 256;                       // of a launch that cuts
 constexpr int kLeastStages = 8;                          // of a part
@@ -35,76 +36,144 @@ struct TilePiece {
     int runs, at, item;                                  // part `at` of up to `runs`; the item of the first
 };
 
-// With a place for every part: each wave holds all requests, K to a lane.  What is cut comes first.
+// Sum over the lanes of a wave, in all of them.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float shifted(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, ROWS, 0xF, false)); }
+__device__ __forceinline__ float wave_sum(float x)
+{
+    x += shifted<0x111, 0xF>(x);                         // as wave_scan
+    x += shifted<0x112, 0xF>(x);
+    x += shifted<0x114, 0xF>(x);
+    x += shifted<0x118, 0xF>(x);
+    x += shifted<0x142, 0xA>(x);
+    x += shifted<0x143, 0xC>(x);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+
+// How a launch that cuts divides its work, by every wave for itself, K consecutive requests per lane.
+template <int K>
+struct TilePlan {
+    int first[K], count[K], ctx[K], tiles[K], runs[K];   // first row, new tokens, length; tiles, and parts of each (1: not cut)
+
+    __device__ __forceinline__ TilePlan(const WindowArgs &w, const Tiling &c, int WT)
+    {
+        const DecodeArgs &a = w.d;
+        const int lane = threadIdx.x & 63;
+        int stages[K];
+        float work = 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int i = min(K * lane + k, a.batch - 1);
+            first[k] = w.q_start[i];
+            count[k] = w.q_start[i + 1];
+            ctx[k] = a.ctx_lens[i];
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            count[k] -= first[k];
+            // (a context shorter than its new tokens, or longer than the table row: nothing is read or written for it; rows past the last: none)
+            const bool on = K * lane + k < a.batch && first[k] >= 0 && count[k] > 0 && ctx[k] >= count[k] && ctx[k] <= a.max_blocks * a.block_size;
+            const int rows = on ? min(count[k], w.total_tokens - first[k]) : 0;
+            tiles[k] = max(0, (rows + WT - 1) / WT);
+            const int p = ctx[k] - count[k] + rows;      // (the last tile's end, and what its first token sees)
+            stages[k] = tiles[k] > 0 ? Sight<32>(p, max(0, p - min(rows, WT) - w.window + 1), w.sinks, std::true_type{}).units : 0;
+            work += (float)stages[k] * (float)tiles[k];
+        }
+        // an even share (the sum is off by a few times 2^-24)
+        const float even = wave_sum(work) * (float)a.num_kv_heads / (float)c.places * 1.00001f + 1.0f;
+        const int size = max(kLeastStages, even < (float)(1 << 26) ? (int)even : 1 << 26), worth = size + size / 2;
+#pragma unroll
+        for (int k = 0; k < K; ++k) runs[k] = stages[k] > worth ? (int)((unsigned)(stages[k] + size - 1) / (unsigned)size) : 1;
+    }
+    __device__ __forceinline__ bool cut(int k) const { return runs[k] > 1; }
+    // Request k of lane l.
+    __device__ __forceinline__ void take(int k, int l, TilePiece &x) const
+    {
+        x.r = K * l + k;
+        x.first = __builtin_amdgcn_readlane(first[k], l);
+        x.n_new = __builtin_amdgcn_readlane(count[k], l);
+        x.ctx = __builtin_amdgcn_readlane(ctx[k], l);
+        x.runs = __builtin_amdgcn_readlane(runs[k], l);
+    }
+};
+// The number of request (k of lane l) that `at` falls to, `at` of its own then: mine[k] of each.
+template <int K>
+__device__ __forceinline__ bool find_request(const int (&mine)[K], int &at, int &k_of, int &l_of)
+{
+    int own = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) own += mine[k];
+    const int upto = wave_scan(own);
+    if (at >= __builtin_amdgcn_readlane(upto, 63)) return false;
+    l_of = __popcll(__ballot(upto <= at));
+    at -= __builtin_amdgcn_readlane(upto - own, l_of);
+    k_of = -1;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int n = __builtin_amdgcn_readlane(mine[k], l_of);
+        if (k_of < 0) {
+            if (at < n) k_of = k; else at -= n;
+        }
+    }
+    return true;
+}
+// The piece'th of all parts, cut requests' first, of each request the longest tile first.
 template <int K>
 __device__ __forceinline__ bool find_tile(const WindowArgs &w, const Tiling &c, int WT, int piece, TilePiece &x)
 {
-    const DecodeArgs &a = w.d;
-    const int lane = threadIdx.x & 63;
-    int first[K], count[K], ctx[K], tiles[K], stages[K], own[K], mine[2] = {0, 0};
-    float work = 0.0f;
-    int longest = 0;
+    const TilePlan<K> plan(w, c, WT);
+    int cuts[K], others[K], sum = 0, at = piece, k_of = 0, l_of = 0;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const int i = min(K * lane + k, a.batch - 1);
-        first[k] = w.q_start[i];
-        count[k] = w.q_start[i + 1];
-        ctx[k] = a.ctx_lens[i];
+        cuts[k] = plan.cut(k) ? plan.tiles[k] * plan.runs[k] : 0;
+        others[k] = plan.cut(k) ? 0 : plan.tiles[k];
+        sum += cuts[k];
     }
+    const int all = __builtin_amdgcn_readlane(wave_scan(sum), 63);
+    if (piece >= all) at -= all;
+    if (!(piece < all ? find_request<K>(cuts, at, k_of, l_of) : find_request<K>(others, at, k_of, l_of))) return false;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        count[k] -= first[k];
-        // (a context shorter than its new tokens, or longer than the table row: nothing is read or written for it; rows past the last: none)
-        const bool on = K * lane + k < a.batch && first[k] >= 0 && count[k] > 0 && ctx[k] >= count[k] && ctx[k] <= a.max_blocks * a.block_size;
-        const int rows = on ? min(count[k], w.total_tokens - first[k]) : 0;
-        tiles[k] = max(0, (rows + WT - 1) / WT);
-        const int p = ctx[k] - count[k] + rows;          // (the last tile's end, and what its first token sees)
-        stages[k] = tiles[k] > 0 ? Sight<32>(p, max(0, p - min(rows, WT) - w.window + 1), w.sinks, std::true_type{}).units : 0;
-        work += (float)stages[k] * (float)tiles[k];
-        longest = max(longest, stages[k]);
-    }
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) work += __shfl_xor(work, s);
-    longest = __builtin_amdgcn_readlane(wave_max_to(longest), 63);
-    // an even share (the sum is off by a few times 2^-24)
-    const float even = work * (float)a.num_kv_heads / (float)c.places * 1.00001f + 1.0f;
-    const int size = max(kLeastStages, even < (float)(1 << 26) ? (int)even : 1 << 26), worth = size + size / 2;
-    // the cut requests' pieces, then the others'
-    bool cut[K];
-    int runs[K];
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        cut[k] = stages[k] > worth;
-        runs[k] = cut[k] ? (int)((unsigned)(stages[k] + size - 1) / (unsigned)size) : 1;
-        own[k] = tiles[k] * runs[k];
-        mine[cut[k] ? 0 : 1] += own[k];
-    }
-    const int upto_cut = wave_scan(mine[0]), cuts = __builtin_amdgcn_readlane(upto_cut, 63);
-    const bool in_cuts = piece < cuts;
-    const int upto = in_cuts ? upto_cut : wave_scan(mine[1]) + cuts;
-    if (piece >= __builtin_amdgcn_readlane(upto, 63)) return false;
-    const int l = __popcll(__ballot(upto <= piece));
-    int at = piece - __builtin_amdgcn_readlane(upto - (in_cuts ? mine[0] : mine[1]), l);
-    bool found = false;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int n = __builtin_amdgcn_readlane(cut[k] == in_cuts ? own[k] : 0, l);
-        if (!found && at < n) {
-            found = true;
-            x.r = K * l + k;
-            x.first = __builtin_amdgcn_readlane(first[k], l);
-            x.n_new = __builtin_amdgcn_readlane(count[k], l);
-            x.ctx = __builtin_amdgcn_readlane(ctx[k], l);
-            x.runs = __builtin_amdgcn_readlane(runs[k], l);
-            const int t = (int)((unsigned)at / (unsigned)x.runs), all = __builtin_amdgcn_readlane(tiles[k], l);
+    for (int k = 0; k < K; ++k)
+        if (k == k_of) {
+            plan.take(k, l_of, x);
+            const int t = (int)((unsigned)at / (unsigned)x.runs);
             x.at = at - t * x.runs;
             x.item = piece - x.at;
-            x.tile = all - 1 - t;                        // (the longest first)
-        } else if (!found) {
-            at -= n;
+            x.tile = __builtin_amdgcn_readlane(plan.tiles[k], l_of) - 1 - t;
+        }
+    return true;
+}
+// The nth tile that is cut: its request, and the number of its first part.
+template <int K>
+__device__ __forceinline__ bool find_cut_tile(const WindowArgs &w, const Tiling &c, int WT, int nth, TilePiece &x)
+{
+    const TilePlan<K> plan(w, c, WT);
+    int cuts[K], own = 0, at = nth, k_of = 0, l_of = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        cuts[k] = plan.cut(k) ? plan.tiles[k] : 0;
+        own += cuts[k] * plan.runs[k];
+    }
+    if (!find_request<K>(cuts, at, k_of, l_of)) return false;
+    int before = __builtin_amdgcn_readlane(wave_scan(own) - own, l_of);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        if (k < k_of) before += __builtin_amdgcn_readlane(cuts[k] * plan.runs[k], l_of);
+        if (k == k_of) {
+            plan.take(k, l_of, x);
+            x.at = 0;
+            x.item = before + at * x.runs;
+            x.tile = __builtin_amdgcn_readlane(plan.tiles[k], l_of) - 1 - at;
         }
     }
-    return found;
+    return true;
+}
+// Stages of each part of a tile of `units`, and parts that there are then: one of earlier tokens may have fewer stages than the request's last one, by which
+// the parts are counted.
+__device__ __forceinline__ int2 parts_of(int units, int runs)
+{
+    const int want = max(1, min(runs, units / (kLeastStages / 2))), each = (int)((unsigned)(units + want - 1) / (unsigned)want);
+    return make_int2(each, (int)((unsigned)(units + each - 1) / (unsigned)each));
 }
 
 // Without: any number of requests, none cut.
@@ -126,18 +195,18 @@ __device__ __forceinline__ bool find_whole_tile(const WindowArgs &w, int WT, int
 
 constexpr size_t tile_state(int D, int columns) { return (size_t)columns * (D + 2); }   // floats
 
-template <int D, int kCB, bool WINDOW>
+template <int D, int kCB, int PS, bool WINDOW>
 __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_tiles(const WindowArgs w, const Tiling c)
 {
-    constexpr int kCols = 16 * kCB, NK = D / 32, NS = D / 16;
+    constexpr int kCols = 16 * kCB, CG = kWaves / PS, NK = D / 32, NS = D / 16;   // columns of a wave; waves with columns of their own
     constexpr int SUBK = 16 * D * 2, VOFF = 2 * SUBK, STAGE = 4 * SUBK;   // bytes of a sub-tile of keys, where values begin, of a stage
     constexpr bool kHold = D <= 128;                     // operands of a stage are held in registers
-    __shared__ __align__(16) char lds[2 * STAGE];
+    __shared__ __align__(16) char lds[2 * PS * STAGE];
     constexpr int SUBS = D == 256 ? 2 : 1, KINDS = D == 64 ? 1 : 2;   // of a thread's units: sub-tiles, keys and values
-    __shared__ uint32_t wild_at[2][kWaves * SUBS];
+    __shared__ uint32_t wild_at[2 * PS][kWaves * SUBS];
 
     const DecodeArgs &a = w.d;
-    const int G = a.num_q_heads / a.num_kv_heads, TW = kCols / G, WT = kWaves * TW;
+    const int G = a.num_q_heads / a.num_kv_heads, TW = kCols / G, WT = CG * TW;
     TilePiece at;
     // (heads next to each other: with 8 of them and more all tiles of one go to one XCD, whose L2 has its keys and values)
     const int piece = __builtin_amdgcn_readfirstlane((int)((unsigned)blockIdx.x / (unsigned)a.num_kv_heads));
@@ -152,17 +221,17 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
     const auto position = [&](int st) { return WINDOW ? see.at(st) : st * 32; };
     int st0 = 0, st1 = see.units, runs = 1;
     if (at.runs > 1) {
-        // (a tile of earlier tokens may have less than the request's last one, by which the parts are counted)
-        const int want = max(1, min(at.runs, see.units / (kLeastStages / 2))), each = (see.units + want - 1) / want;
-        runs = (see.units + each - 1) / each;
+        const int2 parts = parts_of(see.units, at.runs);
+        runs = parts.y;
         if (at.at >= runs) return;
-        st0 = at.at * each;
-        st1 = min(see.units, st0 + each);
+        st0 = at.at * parts.x;
+        st1 = min(see.units, st0 + parts.x);
     }
     st0 = __builtin_amdgcn_readfirstlane(st0);
     st1 = __builtin_amdgcn_readfirstlane(st1);
     // the wave's own tokens; none: positions that see nothing
-    const int wave_tok = at.tile * WT + wv * TW;
+    const int cg = wv / PS, ps = wv % PS;                // its columns, and which of PS stages it takes
+    const int wave_tok = at.tile * WT + cg * TW;
     const bool none = wave_tok >= n_new;
     const int wave_min = __builtin_amdgcn_readfirstlane(none ? 0x3fffffff : base_pos + wave_tok);
     const int wave_max = __builtin_amdgcn_readfirstlane(none ? -1 : base_pos + min(n_new, wave_tok + TW) - 1);
@@ -182,7 +251,7 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
     struct Places {
         uint32_t block[SUBS], at[SUBS];                  // where a sub-tile is: a block, and where in its tile
     };
-    const auto lookup = [&](int st) {
+    const auto lookup = [&](int st) __attribute__((always_inline)) {
         const int t = position(min(st, last_stage));
         Places x;
 #pragma unroll
@@ -201,18 +270,20 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
         }
         return x;
     };
-    uint4 raw[SUBS][KINDS];
-    float2 scale_of[SUBS];
-    const auto load = [&](const Places &x) {
+    struct Codes {
+        uint4 raw[SUBS][KINDS];
+        float2 scale[SUBS];
+    };
+    const auto load = [&](const Places &x, Codes &y) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < SUBS; ++i) {
             const uint64_t block = (uint64_t)x.block[i] * stride, off = block + x.at[i];
-            scale_of[i] = __builtin_bit_cast(float2, *(scales_ptr)(uintptr_t)(sp + block));
+            y.scale[i] = __builtin_bit_cast(float2, *(scales_ptr)(uintptr_t)(sp + block));
             if constexpr (KINDS == 2) {
-                raw[i][0] = *reinterpret_cast<const uint4 *>(kp + off + u16);
-                raw[i][1] = *reinterpret_cast<const uint4 *>(vp + off + u16);
+                y.raw[i][0] = *reinterpret_cast<const uint4 *>(kp + off + u16);
+                y.raw[i][1] = *reinterpret_cast<const uint4 *>(vp + off + u16);
             } else {
-                raw[i][0] = *reinterpret_cast<const uint4 *>((wave_kind ? vp : kp) + off + u16);
+                y.raw[i][0] = *reinterpret_cast<const uint4 *>((wave_kind ? vp : kp) + off + u16);
             }
         }
     };
@@ -220,7 +291,7 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
     // become zeros; whether one that is left is NaN matters where a stage is not seen by all.
     const int wg_min = p_first, wg_hi = p_last - w.window + 1;
     const uint32_t key_to = (u >> 4) * 512 + (u & 15) * 16, value_to = VOFF + ((u >> 6) * 256 + (u >> 4 & 3) * 16 + (u & 15)) * 16;
-    const auto put = [&](int st, int buf) {
+    const auto put = [&](int st, int buf, const Codes &from) __attribute__((always_inline)) {
         char *to = lds + buf * STAGE;
         const int t0 = position(min(st, last_stage));
         const bool edge = (t0 + 31 > wg_min) | (WINDOW && t0 < wg_hi);
@@ -229,14 +300,14 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
 #pragma unroll
             for (int k = 0; k < KINDS; ++k) {
                 const int sub = SUBS == 2 ? i : wave_sub;
-                const uint4 y = raw[i][k];
+                const uint4 y = from.raw[i][k];
                 if (KINDS == 2 ? k == 0 : wave_kind == 0) {
-                    const float s = scale_of[i].x;
+                    const float s = from.scale[i].x;
                     uint4 *p = reinterpret_cast<uint4 *>(to + sub * SUBK + key_to);
                     p[0] = make_uint4(from_codes<false>(y.x, s), from_codes<true>(y.x, s), from_codes<false>(y.y, s), from_codes<true>(y.y, s));
                     p[16] = make_uint4(from_codes<false>(y.z, s), from_codes<true>(y.z, s), from_codes<false>(y.w, s), from_codes<true>(y.w, s));
                 } else {
-                    const float s = scale_of[i].y;
+                    const float s = from.scale[i].y;
                     uint32_t x[4] = {y.x, y.y, y.z, y.w};
                     if (edge) {                          // uniform
                         int left = see.end - (t0 + 16 * sub + (u >> 4 & 3) * 4);   // of the unit's four positions
@@ -263,13 +334,30 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
 
     if (lane == 0) {
 #pragma unroll
-        for (int i = 0; i < SUBS; ++i) wild_at[0][kWaves * i + wv] = wild_at[1][kWaves * i + wv] = 0;
+        for (int i = 0; i < SUBS; ++i) for (int k = 0; k < 2 * PS; ++k) wild_at[k][kWaves * i + wv] = 0;
     }
-    Places next = {};
+    // A round of the walk is PS stages, one for each of the waves that share columns.  The first rounds' codes are asked for together, in front of the queries, and from
+    // there on two rounds ahead of their conversion (one ahead, codes out of memory and not of an L2 are waited for: AAA us, BBB so).
+    Places next[PS];
+    Codes codes[PS], ahead[PS];
+    const auto lookup_round = [&](int st) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < PS; ++k) next[k] = lookup(st + k);
+    };
+    const auto load_round = [&](Codes (&x)[PS]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < PS; ++k) load(next[k], x[k]);
+    };
+    const auto put_round = [&](int st, int buf, const Codes (&x)[PS]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < PS; ++k) put(st + k, buf * PS + k, x[k]);
+    };
     if (st0 < st1) {
-        const Places now = lookup(st0);
-        next = lookup(st0 + 1);
-        load(now);
+        lookup_round(st0);
+        load_round(codes);
+        lookup_round(st0 + PS);
+        load_round(ahead);
+        lookup_round(st0 + 2 * PS);
     }
 
     // this lane's column in each block: (token, head), its position, its queries (of a negative scale: their negatives)
@@ -313,7 +401,7 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
     // The weights of block b, by the reference that it has; the largest of them, found by packed maxima of pairs: they are not negative, so their bits compare as
     // they do, and as those of fp16 numbers.  One of 2^kSlack and more, or no finite one, asks for another reference: rare after the first stages.
     typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
-    const auto weigh = [&](int b) {
+    const auto weigh = [&](int b) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             pw[b][e] = (__bf16)fast_exp2(fmaf(sc0[b][e], scale, -m[b]));
@@ -331,7 +419,7 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
         constexpr unsigned short kBelow = ((127 + (int)kSlack) << 7) - 1;   // the bf16 in front of 2^kSlack
         return __any(__builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, most), u16x2{kBelow, kBelow})) != 0);
     };
-    const auto softmax = [&](int t0, bool masked) {
+    const auto softmax = [&](int t0, bool masked) __attribute__((always_inline)) {
         if (masked) {
 #pragma unroll
             for (int b = 0; b < kCB; ++b)
@@ -372,7 +460,7 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
 
     // A value that is NaN must not reach the columns that do not see it, and a zero weight does not silence it: where a stage that is seen in part has one,
     // the products are taken without, and those of (is NaN) by (is seen) tell which outputs it makes NaN.
-    const auto set_apart = [&](int s, int t0, uint4 &v) {
+    const auto set_apart = [&](int s, int t0, uint4 &v) __attribute__((always_inline)) {
         uint32_t x[4] = {v.x, v.y, v.z, v.w}, is[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -402,7 +490,7 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
     uint4 vheld[kHold ? NS : 1];
     const char *mine = lds + lane * 16;                  // (unit qd * 16 + j)
     const auto key = [&](const char *buf, int i, int h) { return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(buf + h * SUBK + i * 1024)); };
-    const auto read_k = [&](const char *buf) {
+    const auto read_k = [&](const char *buf) __attribute__((always_inline)) {
         if constexpr (kHold) {
 #pragma unroll
             for (int i = 0; i < NK; ++i)
@@ -411,30 +499,35 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
         }
     };
     if (st0 < st1) {
-        put(st0, 0);
-        load(next);
-        next = lookup(st0 + 2);
+        put_round(st0, 0, codes);
         if constexpr (kHold) {
-            put(st0 + 1, 1);                             // (past the last stage: the last one once more, which nobody reads)
-            load(next);
-            next = lookup(st0 + 3);
+            load_round(codes);
+            lookup_round(st0 + 3 * PS);
+            put_round(st0 + PS, 1, ahead);               // (past the last stage: the last one once more, which nobody reads)
+            load_round(ahead);
+            lookup_round(st0 + 4 * PS);
+        } else {
+            load_round(codes);
+            lookup_round(st0 + 3 * PS);
         }
     }
     if constexpr (kHold) {
         __syncthreads();
-        if (st0 < st1) read_k(mine);
+        if (st0 < st1) read_k(mine + ps * STAGE);
     }
-    for (int st = st0; st < st1; ++st) {
-        const int cur = (st - st0) & 1;
+    // The round from stage rd on, whose buffer is `cur`; x: the codes that it converts, and then asks for others.
+    const auto round = [&](int rd, auto parity, Codes (&x)[PS]) __attribute__((always_inline)) {
+        constexpr int cur = parity;
         if constexpr (!kHold) {
             __syncthreads();
-            put(st + 1, cur ^ 1);
-            load(next);
-            next = lookup(st + 3);
+            put_round(rd + PS, cur ^ 1, x);
+            load_round(x);
+            lookup_round(rd + 4 * PS);
         }
-        const char *buf = mine + cur * STAGE;
-        const int t0 = position(st);
-        const bool live = (t0 <= wave_max) & (!WINDOW | (t0 + 31 >= wave_lo) | (t0 < w.sinks));   // uniform over the wave, as what follows
+        const int st = rd + ps;
+        const char *buf = mine + (cur * PS + ps) * STAGE;
+        const int t0 = position(PS > 1 ? min(st, last_stage) : st);
+        const bool live = (t0 <= wave_max) & (!WINDOW | (t0 + 31 >= wave_lo) | (t0 < w.sinks)) & (PS == 1 | st < st1);   // uniform over the wave, as what follows
         const bool masked = !((t0 + 31 <= wave_min) & (!WINDOW | (t0 >= wave_hi) | (t0 + 32 <= w.sinks)));
         const auto values = [&](int s) { return *reinterpret_cast<const uint4 *>(buf + VOFF + s * 1024); };
         const auto vop = [&](int s) { return kHold ? vheld[kHold ? s : 0] : values(s); };
@@ -462,7 +555,7 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
             if (masked) {
                 uint32_t any = 0;
 #pragma unroll
-                for (int k = 0; k < kWaves * SUBS; ++k) any |= wild_at[cur][k];
+                for (int k = 0; k < kWaves * SUBS; ++k) any |= wild_at[cur * PS + ps][k];
                 apart = __builtin_amdgcn_readfirstlane(any) != 0;
             }
             if constexpr (kHold) {
@@ -474,12 +567,12 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
         }
         if constexpr (kHold) {
             __syncthreads();
-            read_k(mine + (cur ^ 1) * STAGE);
-            put(st + 2, cur);
-            load(next);
-            next = lookup(st + 4);
+            read_k(mine + ((cur ^ 1) * PS + ps) * STAGE);
+            put_round(rd + 2 * PS, cur, x);
+            load_round(x);
+            lookup_round(rd + 5 * PS);
         }
-        if (!live) continue;
+        if (!live) return;
 #pragma unroll
         for (int b = 0; b < kCB; ++b) l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pw[b], l[b], 0, 0, 0);
 #pragma unroll
@@ -489,27 +582,79 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
 #pragma unroll
             for (int b = 0; b < kCB; ++b) o[b][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), pw[b], o[b][s], 0, 0, 0);
         }
+    };
+    // (heads of 256: the first round is converted by itself, and the second's codes come first)
+    for (int rd = st0; rd < st1; rd += 2 * PS) {
+        round(rd, std::integral_constant<int, 0>{}, kHold ? codes : ahead);
+        if (rd + PS < st1) round(rd + PS, std::integral_constant<int, 1>{}, kHold ? ahead : codes);
     }
     // (the last products are there before what adds them up or stores them: see window_tiles.h)
     asm volatile("s_nop 7" ::: "memory");
 #pragma unroll
     for (int b = 0; b < kCB; ++b) asm volatile("" : "+v"(l[b]), "+v"(o[b][NS - 1]));
 
+    if constexpr (PS > 1) {
+        // the waves of the same columns: their states through LDS to the first of them
+        constexpr int kState = kCols * (D + 2) * 4;      // bytes
+        static_assert(CG * (PS - 1) * kState <= 2 * PS * STAGE, "the states fit into the stages' place");
+        __syncthreads();
+        char *there = lds + (cg * (PS - 1) + ps - 1) * kState + lane * 16;
+        if (ps > 0 && !none) {
+#pragma unroll
+            for (int b = 0; b < kCB; ++b) {
+#pragma unroll
+                for (int s = 0; s < NS; ++s) *reinterpret_cast<f32x4 *>(there + (b * NS + s) * 1024) = o[b][s];
+                if (qd == 0) *reinterpret_cast<float2 *>(there - lane * 16 + kCols * D * 4 + (b * 16 + j) * 8) = make_float2(m[b], l[b][0]);
+            }
+        }
+        __syncthreads();
+        if (ps == 0 && !none) {
+#pragma unroll
+            for (int k = 0; k < PS - 1; ++k)
+#pragma unroll
+                for (int b = 0; b < kCB; ++b) {
+                    const char *from = lds + (cg * (PS - 1) + k) * kState;
+                    const float2 ml = *reinterpret_cast<const float2 *>(from + kCols * D * 4 + (b * 16 + j) * 8);
+                    const float Mn = fmaxf(m[b], ml.x), f0 = fast_exp2(m[b] - Mn), f = fast_exp2(ml.x - Mn);
+                    m[b] = Mn;
+                    l[b][0] = l[b][0] * f0 + ml.y * f;
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) {
+                        const f32x4 y = *reinterpret_cast<const f32x4 *>(from + lane * 16 + (b * NS + s) * 1024);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[b][s][e] = o[b][s][e] * f0 + y[e] * f;
+                    }
+                }
+        }
+    }
+    const bool holds = ps == 0 && !none;                 // the wave has a state to hand on
     if (runs == 1) {
+        if (PS > 1 && !holds) return;
 #pragma unroll
         for (int b = 0; b < kCB; ++b) store_column<NS>(static_cast<uint16_t *>(a.out) + orow[b], qd, pos[b] >= 0, 1.0f / l[b][0], o[b]);
         return;
     }
-    // the columns of each block as the wave holds them, and their (reference, sum); the last part to arrive adds them up
-    constexpr int kAll = kWaves * kCols;
+    // the columns of each block as the wave holds them, and their (reference, sum); the last part to arrive adds them up, or a second launch
+    constexpr int kAll = CG * kCols;
     constexpr size_t state = tile_state(D, kAll);
     const size_t item = (size_t)at.item * a.num_kv_heads + g, step = (size_t)a.num_kv_heads * state;
     float *first_part = a.partials + item * state, *to = first_part + at.at * step;
-    uint64_t *flags = reinterpret_cast<uint64_t *>(a.partials + (size_t)c.items * state) + item;
-    if (!none) {
+    if (c.later) {                                       // (a second launch adds them up)
+        if (!holds) return;
 #pragma unroll
         for (int b = 0; b < kCB; ++b) {
-            const int block = wv * kCB + b;
+            const int block = cg * kCB + b;
+#pragma unroll
+            for (int s = 0; s < NS; ++s) *reinterpret_cast<f32x4 *>(to + block * 16 * D + s * 256 + 4 * lane) = o[b][s];
+            if (qd == 0) *reinterpret_cast<float2 *>(to + kAll * D + 2 * (block * 16 + j)) = make_float2(m[b], l[b][0]);
+        }
+        return;
+    }
+    uint64_t *flags = reinterpret_cast<uint64_t *>(a.partials + (size_t)c.items * state) + item;
+    if (holds) {
+#pragma unroll
+        for (int b = 0; b < kCB; ++b) {
+            const int block = cg * kCB + b;
 #pragma unroll
             for (int s = 0; s < 2 * NS; ++s)
                 put_shared(to + block * 16 * D + s * 128 + 2 * lane, o[b][s >> 1][2 * (s & 1)], o[b][s >> 1][2 * (s & 1) + 1]);
@@ -524,11 +669,11 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
         if (lane == 0) *is_last = all;
     }
     __syncthreads();
-    if (!*is_last || none) return;
+    if (!*is_last || !holds) return;
     // the parts in order, whichever workgroup this is: bit-reproducible
 #pragma unroll 1
     for (int b = 0; b < kCB; ++b) {
-        const int block = wv * kCB + b;
+        const int block = cg * kCB + b;
         float M = kLeast, L = 0.0f;
         f32x4 A[NS];
 #pragma unroll
@@ -555,6 +700,87 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
     }
 }
 
+// Adds the parts of a tile up behind a launch with `later`: a workgroup takes a block of 16 columns, its waves every fourth part.
+template <int D, int kCB, int CG, bool WINDOW>
+__global__ __launch_bounds__(kThreads) void kv8_join(const WindowArgs w, const Tiling c)
+{
+    constexpr int kCols = 16 * kCB, kAll = CG * kCols, NS = D / 16, N = D >= 256 ? 1 : 2, SLABS = D == 64 ? 2 : NS / kWaves;
+    __shared__ __align__(16) float sums[kWaves][16 * D];
+    __shared__ float2 stats[kWaves][16];
+    const DecodeArgs &a = w.d;
+    const int G = a.num_q_heads / a.num_kv_heads, TW = kCols / G, WT = CG * TW;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 15, qd = lane >> 4;
+    const int nth = __builtin_amdgcn_readfirstlane((int)((unsigned)blockIdx.x / (unsigned)a.num_kv_heads)), g = blockIdx.x - nth * a.num_kv_heads, block = blockIdx.y;
+    TilePiece at;
+    if (a.batch <= 64 ? !find_cut_tile<1>(w, c, WT, nth, at) : !find_cut_tile<4>(w, c, WT, nth, at)) return;
+    const int base_pos = at.ctx - at.n_new, n_new = min(at.n_new, w.total_tokens - at.first), wave_tok = at.tile * WT + block / kCB * TW;
+    if (wave_tok >= n_new) return;                       // (the wave had no tokens and has left nothing)
+    const int p_first = base_pos + at.tile * WT, p_last = base_pos + min(n_new, (at.tile + 1) * WT) - 1;
+    const Sight<32> see(p_last + 1, WINDOW ? max(0, p_first - w.window + 1) : 0, WINDOW ? w.sinks : 0, std::true_type{});
+    const int runs = parts_of(see.units, at.runs).y;
+    if (runs == 1) return;                               // (written already)
+    constexpr size_t state = tile_state(D, kAll);
+    const size_t step = (size_t)a.num_kv_heads * state;
+    const float *parts = a.partials + ((size_t)at.item * a.num_kv_heads + g) * state;
+    float M = kLeast, L = 0.0f;
+    f32x4 A[NS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) A[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int p0 = wv; p0 < runs; p0 += N * kWaves) {
+        float2 ml[N];
+        f32x4 y[N][NS];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float *from = parts + (size_t)min(p0 + k * kWaves, runs - 1) * step;
+            ml[k] = *reinterpret_cast<const float2 *>(from + kAll * D + 2 * (block * 16 + j));
+#pragma unroll
+            for (int s = 0; s < NS; ++s) y[k][s] = *reinterpret_cast<const f32x4 *>(from + block * 16 * D + s * 256 + 4 * lane);
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            if (p0 + k * kWaves >= runs) break;          // uniform
+            const float Mn = fmaxf(M, ml[k].x), f0 = fast_exp2(M - Mn), f = fast_exp2(ml[k].x - Mn);
+            L = L * f0 + ml[k].y * f;
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) A[s][e] = A[s][e] * f0 + y[k][s][e] * f;
+            M = Mn;
+        }
+    }
+#pragma unroll
+    for (int s = 0; s < NS; ++s) *reinterpret_cast<f32x4 *>(&sums[wv][s * 256 + 4 * lane]) = A[s];
+    if (qd == 0) stats[wv][j] = make_float2(M, L);
+    __syncthreads();
+    // each wave some of the outputs, the parts' sums in order
+    if (wv * SLABS >= NS) return;
+    float2 ml[kWaves];
+    M = kLeast;
+    L = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+        ml[k] = stats[k][j];
+        M = fmaxf(M, ml[k].x);
+    }
+    f32x4 B[SLABS];
+#pragma unroll
+    for (int s = 0; s < SLABS; ++s) B[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+        const float f = fast_exp2(ml[k].x - M);
+        L += ml[k].y * f;
+#pragma unroll
+        for (int s = 0; s < SLABS; ++s) {
+            const f32x4 y = *reinterpret_cast<const f32x4 *>(&sums[k][(wv * SLABS + s) * 256 + 4 * lane]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) B[s][e] += y[e] * f;
+        }
+    }
+    const int col = block % kCB * 16 + j, tl = col / G, tok = wave_tok + tl;
+    const bool ok = col < TW * G && tok < n_new;
+    store_column<SLABS>(static_cast<uint16_t *>(a.out) + ((size_t)(at.first + (ok ? tok : 0)) * a.num_q_heads + g * G + (ok ? col - tl * G : 0)) * D + 16 * wv * SLABS, qd, ok, 1.0f / L, B);
+}
+
 // A wavefront per token and kv head (or pass), weights as pairs of bf16: for more than 32 heads to a kv head, and where a caller asks for it.
 template <int D>
 __global__ __launch_bounds__(kThreads, D >= 256 ? 1 : 2) void kv8_rows(const WindowArgs w)
@@ -575,25 +801,34 @@ __global__ __launch_bounds__(kThreads, D >= 256 ? 1 : 2) void kv8_rows(const Win
     });
 }
 
-template <int D, int kCB>
+template <int D, int kCB, int PS>
 hipError_t launch_tiles(const WindowArgs &w, hipStream_t s)
 {
     const DecodeArgs &a = w.d;
-    const int WT = kWaves * (16 * kCB / (a.num_q_heads / a.num_kv_heads));
+    constexpr int CG = kWaves / PS;
+    const int WT = CG * (16 * kCB / (a.num_q_heads / a.num_kv_heads));
     const long long tiles = (long long)w.total_tokens / WT + a.batch, heads = a.num_kv_heads;
-    Tiling c = {0, 0};
+    Tiling c = {0, 0, 0};
     if (a.batch <= kMostRequests) {
         // Parts are no more than 5 / 3 of the places (see kv8_decode.hip); two workgroups fit a CU.
-        const long long state = (long long)tile_state(D, kWaves * 16 * kCB) * (long long)sizeof(float), room = (long long)a.partial_capacity / (state + 8);
+        const long long state = (long long)tile_state(D, CG * 16 * kCB) * (long long)sizeof(float), room = (long long)a.partial_capacity / (state + 8);
         c.places = (int)std::min(512LL, room * 3 / 5 - 1);
         if (c.places < 1) c.places = 0;
         c.items = (int)std::min(room, 1024LL);
+        // Few tiles, which are cut where contexts are long (a row of fewer stages than one and a half parts cannot be).
+        c.later = c.places > 0 && tiles * heads < 512 && (long long)a.max_blocks * a.block_size > 32 * kLeastStages * 3 / 2;
     }
     const long long grid = (tiles * heads + (c.places > 0 ? 2LL * c.places : 0) + heads - 1) / heads * heads;
     if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
     const bool window = w.window < (long long)a.max_blocks * a.block_size;
-    if (window) hipLaunchKernelGGL((kv8_tiles<D, kCB, true>), dim3((unsigned)grid), dim3(kThreads), 0, s, w, c);
-    else hipLaunchKernelGGL((kv8_tiles<D, kCB, false>), dim3((unsigned)grid), dim3(kThreads), 0, s, w, c);
+    if (window) hipLaunchKernelGGL((kv8_tiles<D, kCB, PS, true>), dim3((unsigned)grid), dim3(kThreads), 0, s, w, c);
+    else hipLaunchKernelGGL((kv8_tiles<D, kCB, PS, false>), dim3((unsigned)grid), dim3(kThreads), 0, s, w, c);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !c.later) return e;
+    // (a tile that is cut has two parts at least)
+    const dim3 join((unsigned)(heads * std::min(tiles, c.places * 5 / 6 / heads + 1)), CG * kCB);
+    if (window) hipLaunchKernelGGL((kv8_join<D, kCB, CG, true>), join, dim3(kThreads), 0, s, w, c);
+    else hipLaunchKernelGGL((kv8_join<D, kCB, CG, false>), join, dim3(kThreads), 0, s, w, c);
     return hipGetLastError();
 }
 
@@ -610,8 +845,13 @@ hipError_t launch(const WindowArgs &w, hipStream_t s)
         hipLaunchKernelGGL(kv8_rows<D>, dim3((unsigned)((items + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, w);
         return hipGetLastError();
     }
-    const bool narrow = G <= 16 && (long long)w.max_new_tokens * G <= 256;
-    return narrow ? launch_tiles<D, 1>(w, s) : launch_tiles<D, 2>(w, s);
+    if constexpr (D >= 256) {
+        // (of 64 columns two workgroups fit a CU, of 128 one: 4 prompts of 1 024, 16 / 4 heads, 88 us and 119)
+        return G <= 16 ? launch_tiles<D, 1, 1>(w, s) : launch_tiles<D, 2, 1>(w, s);
+    } else {
+        const bool narrow = (long long)w.max_new_tokens * G <= 256;
+        return narrow ? launch_tiles<D, 2, 2>(w, s) : launch_tiles<D, 2, 1>(w, s);
+    }
 }
 
 }  // namespace

@@ -182,7 +182,9 @@ def test_requests_that_mean_nothing_are_left_alone():
         small = torch.full((81, 8, 128), 2.5, dtype=torch.bfloat16, device=rig.dev)
         rig.lamps.prefill_attn(1, 1, 7, q.to(rig.dev), rig.ints([0, 20]), rig.ints(table), rig.ints([60]), small, max_new_tokens=most)
         torch.cuda.synchronize()
-        assert (small[7:] == 2.5).all() and torch.equal(small[:7], out[:7])
+        # (a launch of fewer tokens may take other tiles, whose sums have another order: the first seven rows by the formula, as those of a context of 47)
+        assert (small[7:] == 2.5).all()
+        check(rig, 1, q, [(47, 7)], table, [0], small, rounded)
     rig.close()
 
 
