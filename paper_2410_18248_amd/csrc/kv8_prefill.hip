@@ -29,6 +29,7 @@ struct Tiling {
 };
 constexpr int kMostRequests = 256;                       // of a launch that cuts
 constexpr int kLeastStages = 8;                          // of a part
+constexpr int kTries = 12;
 
 // What a workgroup takes.
 struct TilePiece {
@@ -81,9 +82,20 @@ struct TilePlan {
         }
         // an even share (the sum is off by a few times 2^-24)
         const float even = wave_sum(work) * (float)a.num_kv_heads / (float)c.places * 1.00001f + 1.0f;
-        const int size = max(kLeastStages, even < (float)(1 << 26) ? (int)even : 1 << 26), worth = size + size / 2;
+        int size = max(kLeastStages, even < (float)(1 << 26) ? (int)even : 1 << 26);
+        // Where the parts are added up by a second launch they are of about one size, and the chip holds all of them at once: from an even share their size goes up until there are no
+        // more of them than places (12 responses, 853 parts of an even share and up to half as much again on 512 places / 512: 107 us and FILL).
+        for (int tries = c.later ? kTries : 0;; --tries) {
+            const int worth = c.later ? size : size + size / 2;
+            int sum = 0;
 #pragma unroll
-        for (int k = 0; k < K; ++k) runs[k] = stages[k] > worth ? (int)((unsigned)(stages[k] + size - 1) / (unsigned)size) : 1;
+            for (int k = 0; k < K; ++k) {
+                runs[k] = stages[k] > worth ? (int)((unsigned)(stages[k] + size - 1) / (unsigned)size) : 1;
+                sum += tiles[k] * runs[k];
+            }
+            if (tries == 0 || __builtin_amdgcn_readlane(wave_scan(sum), 63) * a.num_kv_heads <= c.places) break;
+            size += size / 16 + 1;
+        }
     }
     __device__ __forceinline__ bool cut(int k) const { return runs[k] > 1; }
     // Request k of lane l.
@@ -810,9 +822,9 @@ hipError_t launch_tiles(const WindowArgs &w, hipStream_t s)
     const long long tiles = (long long)w.total_tokens / WT + a.batch, heads = a.num_kv_heads;
     Tiling c = {0, 0, 0};
     if (a.batch <= kMostRequests) {
-        // Parts are no more than 5 / 3 of the places (see kv8_decode.hip); two workgroups fit a CU.
+        // Parts are no more than twice the places (a range's n / size + 1, where n is more than size); two workgroups fit a CU.
         const long long state = (long long)tile_state(D, CG * 16 * kCB) * (long long)sizeof(float), room = (long long)a.partial_capacity / (state + 8);
-        c.places = (int)std::min(512LL, room * 3 / 5 - 1);
+        c.places = (int)std::min(512LL, room / 2 - 1);
         if (c.places < 1) c.places = 0;
         c.items = (int)std::min(room, 1024LL);
         // Few tiles, which are cut where contexts are long (a row of fewer stages than one and a half parts cannot be).
@@ -826,7 +838,7 @@ hipError_t launch_tiles(const WindowArgs &w, hipStream_t s)
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !c.later) return e;
     // (a tile that is cut has two parts at least)
-    const dim3 join((unsigned)(heads * std::min(tiles, c.places * 5 / 6 / heads + 1)), CG * kCB);
+    const dim3 join((unsigned)(heads * std::min(tiles, c.places / heads + 1)), CG * kCB);
     if (window) hipLaunchKernelGGL((kv8_join<D, kCB, CG, true>), join, dim3(kThreads), 0, s, w, c);
     else hipLaunchKernelGGL((kv8_join<D, kCB, CG, false>), join, dim3(kThreads), 0, s, w, c);
     return hipGetLastError();
