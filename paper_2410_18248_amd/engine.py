@@ -70,7 +70,8 @@ class DeviceSource:
 
 class LiveEngine:
     def __init__(self, cfg, sched_cfg, source, device="cuda:0", observer=None, layered_swap=False, rope=None, windows=None):
-        """cfg: LampsConfig (pools are allocated here); sched_cfg: LampsSchedConfig whose
+        """cfg: LampsConfig (pools are allocated here; LAMPS_E4M3: the source's rows are bf16, the cache is
+        held in 8 bits); sched_cfg: LampsSchedConfig whose
         memory_tokens must not exceed num_blocks * block_size; observer(kind, rid, layer, first_pos,
         out_rows): called with the attention output of every processed token (tests);
         layered_swap: swap layer-major, so that a returning request's first layers run while the
@@ -82,10 +83,10 @@ class LiveEngine:
         self.layered = layered_swap
         self.rope, self.windows = rope, windows or [None] * cfg.num_layers
         assert len(self.windows) == cfg.num_layers
-        self.tdtype = torch.bfloat16 if cfg.dtype == P.LAMPS_BF16 else torch.float32
-        elems = P.lamps_pool_bytes(cfg) // (2 if cfg.dtype == P.LAMPS_BF16 else 4)
-        self.k_pool = torch.zeros(elems, dtype=self.tdtype, device=self.dev)
-        self.v_pool = torch.zeros(elems, dtype=self.tdtype, device=self.dev)
+        if rope is not None and cfg.dtype == P.LAMPS_E4M3:
+            raise ValueError("rotary appends do not go into a cache of 8 bits")
+        self.tdtype = torch.float32 if cfg.dtype == P.LAMPS_F32 else torch.bfloat16     # of the rows
+        self.k_pool, self.v_pool = (torch.zeros(P.lamps_pool_bytes(cfg), dtype=torch.uint8, device=self.dev) for _ in range(2))
         self.ws = torch.empty(P.lamps_workspace_bytes(cfg), dtype=torch.uint8, device=self.dev)
         self.cs, self.so, self.si = (torch.cuda.Stream(self.dev) for _ in range(3))
         torch.cuda.synchronize()

@@ -46,13 +46,17 @@ def main():
     ap.add_argument("--rotary", action="store_true", help="queries and keys are normalised and turned on their way (rotary positions)")
     ap.add_argument("--window", type=int, default=0, help="every other layer sees only the last WINDOW positions and the first --sinks")
     ap.add_argument("--sinks", type=int, default=4)
+    ap.add_argument("--cache", default="bf16", choices=["bf16", "e4m3"], help="what keys and values are held in (e4m3: half the bytes; not with --rotary)")
     a = ap.parse_args()
+    if a.rotary and a.cache == "e4m3":
+        ap.error("--rotary goes with a cache of bf16")
     import torch
     pol = {"fcfs": P.LAMPS_POLICY_FCFS, "sjf": P.LAMPS_POLICY_SJF, "sjf_total": P.LAMPS_POLICY_SJF_TOTAL,
            "lamps": P.LAMPS_POLICY_LAMPS}[a.policy]
     bs, D = 16, 128
     nb = a.memory_tokens // bs + a.requests + 8
-    cfg = P.LampsConfig(a.layers, a.heads, a.kv_heads, D, bs, nb, 256, a.max_batch, P.LAMPS_BF16, 0.0, 0, 0)
+    cfg = P.LampsConfig(a.layers, a.heads, a.kv_heads, D, bs, nb, 256, a.max_batch,
+                        P.LAMPS_E4M3 if a.cache == "e4m3" else P.LAMPS_BF16, 0.0, 0, 0)
     M = float(P.lamps_kv_bytes_per_token(cfg))
     # cost model used for the handling decision and the rank only (time itself is measured)
     cost = P.LampsCostModel(2e-3, 2e-8 * a.layers, 1e-3, 3e-6 * a.layers, 3e-4, 3.7e-7 * a.layers, 0, 0)
@@ -80,7 +84,7 @@ def main():
             mix[x] += 1
     free_ok = eng.lam.num_free() == nb
     out = {"policy": a.policy, "requests": a.requests, "layers": a.layers, "heads": a.heads, "kv_heads": a.kv_heads,
-           "memory_tokens": a.memory_tokens, "wall_s": wall, "scheduler_time_s": eng.sched.now(), **stats,
+           "memory_tokens": a.memory_tokens, "cache": a.cache, "wall_s": wall, "scheduler_time_s": eng.sched.now(), **stats,
            "generated_tokens_per_s": stats["decode_tokens"] / wall,
            "mean_latency_s": float(np.mean(lat)), "p99_latency_s": float(np.percentile(lat, 99)),
            "mean_ttft_s": float(np.mean(ttft)), "handling_preserve_discard_swap": mix,
