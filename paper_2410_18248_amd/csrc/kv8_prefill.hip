@@ -84,7 +84,9 @@ struct TilePlan {
         const float even = wave_sum(work) * (float)a.num_kv_heads / (float)c.places * 1.00001f + 1.0f;
         int size = max(kLeastStages, even < (float)(1 << 26) ? (int)even : 1 << 26);
         // Where the parts are added up by a second launch they are of about one size, and the chip holds all of them at once: from an even share their size goes up until there are no
-        // more of them than places (12 responses, 853 parts of an even share and up to half as much again on 512 places / 512: 107 us and FILL).
+        // more of them than places (12 responses of 4 to 64 tokens on 300 to
+        // 30 000, 32 / 8 heads: 853 parts of an even share and up to half as much again, 114 us; 504 so, 84; the line of all tiles in even shares, the ends of tiles in the middle of
+        // one, 90 to 96: two workgroups of a CU share what they wait for, and a tile's beginning and end cost what 8 stages do).
         for (int tries = c.later ? kTries : 0;; --tries) {
             const int worth = c.later ? size : size + size / 2;
             int sum = 0;
@@ -348,10 +350,10 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
 #pragma unroll
         for (int i = 0; i < SUBS; ++i) for (int k = 0; k < 2 * PS; ++k) wild_at[k][kWaves * i + wv] = 0;
     }
-    // A round of the walk is PS stages, one for each of the waves that share columns.  The first rounds' codes are asked for together, in front of the queries, and from
-    // there on two rounds ahead of their conversion (one ahead, codes out of memory and not of an L2 are waited for: AAA us, BBB so).
+    // A round of the walk is PS stages, one for each of the waves that share columns.  Codes are asked for a round ahead of their conversion, the first in front of the
+    // queries (two rounds ahead is no faster: 12 responses 84 us, 4 prompts of 4 096 1 008, either way).
     Places next[PS];
-    Codes codes[PS], ahead[PS];
+    Codes codes[PS];
     const auto lookup_round = [&](int st) __attribute__((always_inline)) {
 #pragma unroll
         for (int k = 0; k < PS; ++k) next[k] = lookup(st + k);
@@ -368,8 +370,6 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
         lookup_round(st0);
         load_round(codes);
         lookup_round(st0 + PS);
-        load_round(ahead);
-        lookup_round(st0 + 2 * PS);
     }
 
     // this lane's column in each block: (token, head), its position, its queries (of a negative scale: their negatives)
@@ -514,13 +514,13 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
         put_round(st0, 0, codes);
         if constexpr (kHold) {
             load_round(codes);
-            lookup_round(st0 + 3 * PS);
-            put_round(st0 + PS, 1, ahead);               // (past the last stage: the last one once more, which nobody reads)
-            load_round(ahead);
-            lookup_round(st0 + 4 * PS);
-        } else {
+            lookup_round(st0 + 2 * PS);
+            put_round(st0 + PS, 1, codes);               // (past the last stage: the last one once more, which nobody reads)
             load_round(codes);
             lookup_round(st0 + 3 * PS);
+        } else {
+            load_round(codes);
+            lookup_round(st0 + 2 * PS);
         }
     }
     if constexpr (kHold) {
@@ -528,13 +528,13 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
         if (st0 < st1) read_k(mine + ps * STAGE);
     }
     // The round from stage rd on, whose buffer is `cur`; x: the codes that it converts, and then asks for others.
-    const auto round = [&](int rd, auto parity, Codes (&x)[PS]) __attribute__((always_inline)) {
+    const auto round = [&](int rd, auto parity) __attribute__((always_inline)) {
         constexpr int cur = parity;
         if constexpr (!kHold) {
             __syncthreads();
-            put_round(rd + PS, cur ^ 1, x);
-            load_round(x);
-            lookup_round(rd + 4 * PS);
+            put_round(rd + PS, cur ^ 1, codes);
+            load_round(codes);
+            lookup_round(rd + 3 * PS);
         }
         const int st = rd + ps;
         const char *buf = mine + (cur * PS + ps) * STAGE;
@@ -580,9 +580,9 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
         if constexpr (kHold) {
             __syncthreads();
             read_k(mine + ((cur ^ 1) * PS + ps) * STAGE);
-            put_round(rd + 2 * PS, cur, x);
-            load_round(x);
-            lookup_round(rd + 5 * PS);
+            put_round(rd + 2 * PS, cur, codes);
+            load_round(codes);
+            lookup_round(rd + 4 * PS);
         }
         if (!live) return;
 #pragma unroll
@@ -597,8 +597,8 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
     };
     // (heads of 256: the first round is converted by itself, and the second's codes come first)
     for (int rd = st0; rd < st1; rd += 2 * PS) {
-        round(rd, std::integral_constant<int, 0>{}, kHold ? codes : ahead);
-        if (rd + PS < st1) round(rd + PS, std::integral_constant<int, 1>{}, kHold ? ahead : codes);
+        round(rd, std::integral_constant<int, 0>{});
+        if (rd + PS < st1) round(rd + PS, std::integral_constant<int, 1>{});
     }
     // (the last products are there before what adds them up or stores them: see window_tiles.h)
     asm volatile("s_nop 7" ::: "memory");
@@ -827,7 +827,8 @@ hipError_t launch_tiles(const WindowArgs &w, hipStream_t s)
         c.places = (int)std::min(512LL, room / 2 - 1);
         if (c.places < 1) c.places = 0;
         c.items = (int)std::min(room, 1024LL);
-        // Few tiles, which are cut where contexts are long (a row of fewer stages than one and a half parts cannot be).
+        // Few tiles, which are cut where contexts are long (a row of fewer stages than one and a half parts cannot be).  The last part to arrive adds up: the responses 109 us, 16 tokens
+        // on 8 000 49; a second launch: 84 and 21.
         c.later = c.places > 0 && tiles * heads < 512 && (long long)a.max_blocks * a.block_size > 32 * kLeastStages * 3 / 2;
     }
     const long long grid = (tiles * heads + (c.places > 0 ? 2LL * c.places : 0) + heads - 1) / heads * heads;
@@ -861,6 +862,8 @@ hipError_t launch(const WindowArgs &w, hipStream_t s)
         // (of 64 columns two workgroups fit a CU, of 128 one: 4 prompts of 1 024, 16 / 4 heads, 88 us and 119)
         return G <= 16 ? launch_tiles<D, 1, 1>(w, s) : launch_tiles<D, 2, 1>(w, s);
     } else {
+        // (few columns: four waves on 64 of them and two stages at a time.  12 requests of 4 to 64 tokens on 300 to 3 000, 32 plain heads, by 128 and by 64 columns, us: 70
+        // and 46; 16 of 512, 32 / 8 heads: 75 and 109; the responses of above 85 and 84)
         const bool narrow = (long long)w.max_new_tokens * G <= 256;
         return narrow ? launch_tiles<D, 2, 2>(w, s) : launch_tiles<D, 2, 1>(w, s);
     }

@@ -38,8 +38,8 @@ def test_scales_come_by_scalar_loads(code):
 
 
 def test_workgroups_per_cu(kernels):  # noqa: F811
-    least = {"kv8_decodeILi64": 4, "kv8_decodeILi128": 3, "kv8_decodeILi256": 1, "kv8_tilesILi64ELi1": 4, "kv8_tilesILi64ELi2": 2, "kv8_tilesILi128ELi1": 2,
-             "kv8_tilesILi128ELi2": 2, "kv8_tilesILi256ELi1": 2, "kv8_tilesILi256ELi2": 1}
+    least = {"kv8_decodeILi64": 4, "kv8_decodeILi128": 3, "kv8_decodeILi256": 1, "kv8_tilesILi64ELi2ELi2": 3, "kv8_tilesILi64ELi2ELi1": 3,
+             "kv8_tilesILi128ELi2ELi2": 2, "kv8_tilesILi128ELi2ELi1": 2, "kv8_tilesILi256ELi1ELi1": 2, "kv8_tilesILi256ELi2ELi1": 1}
     seen = set()
     for name, k in kernels.items():
         for part, n in least.items():

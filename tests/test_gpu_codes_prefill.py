@@ -26,6 +26,8 @@ FORMS = [
     (8, 1, 64, 16, [(4000, 3), (30, 30), (2500, 40), (700, 1)]),  # walks that are cut
     (16, 2, 256, 16, [(3000, 9), (2000, 2000)]),
     (2, 1, 128, 64, [(9000, 70)]),
+    (32, 2, 128, 16, [(1100, 1100), (1500, 1000), (40, 40)]),     # many tiles
+    (16, 16, 128, 32, [(2100, 2100), (2600, 2050), (1, 1)]),
 ]
 
 
@@ -106,12 +108,11 @@ def test_prefill_window(H, Hkv, D, bs, reqs, window, sinks, most):
     rig.close()
 
 
-@pytest.mark.parametrize("H,Hkv,D", [(8, 2, 128), (4, 4, 64), (8, 4, 256)])
+@pytest.mark.parametrize("H,Hkv,D,c,n,at", [(8, 2, 128, 130, 100, 77), (4, 4, 64, 130, 100, 77), (8, 4, 256, 130, 100, 77), (32, 2, 128, 2200, 2150, 1407)])
 @pytest.mark.parametrize("window", [ALL, 24])
 @pytest.mark.parametrize("most", [0, -1])
-def test_values_that_are_nan_reach_those_that_see_them(H, Hkv, D, window, most):
+def test_values_that_are_nan_reach_those_that_see_them(H, Hkv, D, c, n, at, window, most):
     """One NaN value at a position: rows from there on (in the window) are NaN in its dim and head, others are not; a NaN key: in all dims."""
-    c, n, at = 130, 100, 77
     rig, table = cache(H, Hkv, D, 16, [c], 5)
     q = F.normal(9, n, H, D)
     clean = torch.zeros(n, H, D, dtype=torch.bfloat16, device=rig.dev)
