@@ -5,6 +5,8 @@
 // rounded to the new one.  Scales, codes and the rounding: kv8.h.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "internal.h"
 #include "kv8.h"
 #include "requests.h"
@@ -22,87 +24,99 @@ __device__ __forceinline__ uint32_t wave_most(uint32_t x)
     for (int k = 1; k < 64; k *= 2) x = max(x, (uint32_t)__shfl_xor((int)x, k));
     return x;
 }
+// The same over rows of 16 lanes.
+template <int CTRL>
+__device__ __forceinline__ uint32_t row_max(uint32_t x) { return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true)); }
+__device__ __forceinline__ uint32_t row_most(uint32_t x) { return row_max<0x121>(row_max<0x122>(row_max<0x124>(row_max<0x128>(x)))); }   // (turned by 8, 4, 2, 1 lanes)
 
 // ---------------------------------------------------------------- one token per request
 
-// A wave takes the keys, or the values, of one head; unit 2 g + (0 or 1).  Bound by the launch and the round trips in front of the stores: length,
-// mask and vector are asked for together, then the table entry, then the block's scale.
+// Sixteen lanes take the keys, or the values, of one head; unit 2 g + (0 or 1).  Bound by the launch and the round trips in front of the stores: length,
+// mask and vectors are asked for together, then the table entry, then the block's scales.  256 requests of 40 heads of 128, a tenth of them masked out, us: 6.4 (a wave to a head's
+// keys or values, 18 000 waves on a chip that holds 8 192 of them: 9.0); one request of 8 heads 4.8, of which the kernel is 2.6.
 template <int D>
 __global__ __launch_bounds__(kAdvanceThreads) void kv8_append(const AppendArgs a)
 {
-    constexpr int E = D / 64;                            // dims of a lane
-    const int r = blockIdx.x, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+    constexpr int E = D / 16;                            // dims of a lane
+    const int r = blockIdx.x, lane = threadIdx.x & 63, waves = blockDim.x >> 6, quarter = lane >> 4, d0 = (lane & 15) * E;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), units = 2 * a.num_kv_heads;
-    const int d0 = lane * E;
-    const auto vector = [&](int u, uint32_t (&x)[E]) {   // its dims, as bits
+    const auto vector = [&](int u, uint32_t (&x)[E / 2]) {   // its dims
         const uint16_t *p = static_cast<const uint16_t *>(u & 1 ? a.v_new : a.k_new) + ((size_t)r * a.num_kv_heads + (u >> 1)) * D + d0;
-        if constexpr (E == 1) x[0] = *p;
-        if constexpr (E == 2) {
-            const uint32_t w = *reinterpret_cast<const uint32_t *>(p);
-            x[0] = w & 0xFFFFu; x[1] = w >> 16;
-        }
-        if constexpr (E == 4) {
-            const uint2 w = *reinterpret_cast<const uint2 *>(p);
-            x[0] = w.x & 0xFFFFu; x[1] = w.x >> 16; x[2] = w.y & 0xFFFFu; x[3] = w.y >> 16;
+#pragma unroll
+        for (int e = 0; e < E / 2; e += 2) {
+            const uint2 y = *reinterpret_cast<const uint2 *>(p + 2 * e);
+            x[e] = y.x; x[e + 1] = y.y;
         }
     };
-    int u = blockIdx.y * waves + wv;
-    uint32_t x[E];
-    vector(min(u, units - 1), x);
+    int u0 = (blockIdx.y * waves + wv) * 4;              // the wave's first
+    uint32_t x[E / 2];
+    vector(min(u0 + quarter, units - 1), x);
     const int t = a.ctx_lens[r], running = a.running[r];
     if (!running) return;                                // uniform over the workgroup
-    __syncthreads();
+    if (a.advance) __syncthreads();                      // (all of its waves have read the length)
     const int lb = t >> a.log2_block_size, slot = t & (a.block_size - 1);
     if (t < 0 || lb >= a.max_blocks) return;
     const int block = a.block_table[(size_t)r * a.max_blocks + lb];
     if (block < 0 || block >= a.num_blocks) return;
     const size_t tile = (size_t)a.block_size * D, slice = codes_slice(a.num_kv_heads, a.block_size, D);
     const size_t at = ((size_t)block * a.num_layers + a.layer) * slice;
-    float *scales = reinterpret_cast<float *>(static_cast<char *>(a.k_pool) + at + a.num_kv_heads * tile);
-    for (; u < units; u += waves * gridDim.y) {
-        const float old = slot > 0 ? scales[u] : 0.0f;
+    char *const k_codes = static_cast<char *>(a.k_pool) + at, *const v_codes = static_cast<char *>(a.v_pool) + at;
+    float *scales = reinterpret_cast<float *>(k_codes + a.num_kv_heads * tile);
+    for (; u0 < units; u0 += 4 * waves * gridDim.y) {
+        const int u = u0 + quarter;
+        const bool on = u < units;
+        const float old = on && slot > 0 ? scales[u] : 0.0f;
         uint32_t most = 0;
 #pragma unroll
-        for (int e = 0; e < E; ++e) most = max(most, finite_size(x[e]));
-        const float scale = fmaxf(scale_for(wave_most(most)), old), inv = inverse(scale);
-        char *codes = static_cast<char *>(u & 1 ? a.v_pool : a.k_pool) + at + (u >> 1) * tile;
-        if (slot > 0 && old != scale) {                  // uniform: what is there, by the new scale
-            const float f = old * inv;
-            for (int i = lane; i < ((slot + 15) >> 4) * D; i += 64) {
-                const int sub = i / D, c = i & (D - 1);
-                // a unit of keys is one slot's, of values four slots'
-                const int s0 = sub * 16 + (u & 1 ? (c >> 4 & 3) * 4 : c & 15);
-                if (s0 >= slot) continue;
-                uint4 *p = reinterpret_cast<uint4 *>(codes) + i;
-                const uint4 w = *p;
-                uint4 y = make_uint4(recode(w.x, f), recode(w.y, f), recode(w.z, f), recode(w.w, f));
-                if ((u & 1) && s0 + 4 > slot) {
-                    const uint32_t keep = 0xFFFFFFFFu << (8 * (slot - s0));   // slots that hold nothing: as they were
-                    y.x = (y.x & ~keep) | (w.x & keep);
-                    y.y = (y.y & ~keep) | (w.y & keep);
-                    y.z = (y.z & ~keep) | (w.z & keep);
-                    y.w = (y.w & ~keep) | (w.w & keep);
+        for (int e = 0; e < E / 2; ++e) most = max(most, max(finite_size(x[e]), finite_size(x[e] >> 16)));
+        const float scale = fmaxf(scale_for(row_most(most)), old), inv = inverse(scale);
+        // what is there, by the new scale: the wave together, a unit at a time
+        uint64_t grown = __ballot(on && slot > 0 && old != scale) & 0x0001000100010001ull;
+        if (grown) {                                     // uniform
+            const float factor = old * inv;
+            do {
+                const int from = __builtin_ctzll(grown), v = u0 + (from >> 4);
+                grown &= grown - 1;
+                const float f = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(factor), from));
+                char *codes = (v & 1 ? v_codes : k_codes) + (v >> 1) * tile;
+                for (int i = lane; i < ((slot + 15) >> 4) * D; i += 64) {
+                    const int sub = i / D, c = i & (D - 1);
+                    // a unit of keys is one slot's, of values four slots'
+                    const int s0 = sub * 16 + (v & 1 ? (c >> 4 & 3) * 4 : c & 15);
+                    if (s0 >= slot) continue;
+                    uint4 *p = reinterpret_cast<uint4 *>(codes) + i;
+                    const uint4 w = *p;
+                    uint4 y = make_uint4(recode(w.x, f), recode(w.y, f), recode(w.z, f), recode(w.w, f));
+                    if ((v & 1) && s0 + 4 > slot) {
+                        const uint32_t keep = 0xFFFFFFFFu << (8 * (slot - s0));   // slots that hold nothing: as they were
+                        y.x = (y.x & ~keep) | (w.x & keep);
+                        y.y = (y.y & ~keep) | (w.y & keep);
+                        y.z = (y.z & ~keep) | (w.z & keep);
+                        y.w = (y.w & ~keep) | (w.w & keep);
+                    }
+                    *p = y;
                 }
-                *p = y;
-            }
+            } while (grown);
             __builtin_amdgcn_s_waitcnt(0);               // (the token's own codes lie in the same units)
         }
-        float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        uint32_t w[E / 4];
 #pragma unroll
-        for (int e = 0; e < E; ++e) f[e] = __uint_as_float(x[e] << 16);
-        const uint32_t w = to_codes(f[0], f[1], f[2], f[3], inv);
-        char *sub = codes + (size_t)(slot >> 4) * 16 * D;
-        if (u & 1) {
+        for (int e = 0; e < E / 4; ++e)
+            w[e] = to_codes(__uint_as_float(x[2 * e] << 16), __uint_as_float(x[2 * e] & 0xFFFF0000u), __uint_as_float(x[2 * e + 1] << 16), __uint_as_float(x[2 * e + 1] & 0xFFFF0000u), inv);
+        if (on) {
+            char *sub = (u & 1 ? v_codes : k_codes) + (u >> 1) * tile + (size_t)(slot >> 4) * 16 * D;
+            if (u & 1) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) sub[value_code(slot & 15, d0 + e)] = (char)(w >> (8 * e));
-        } else {
-            char *p = sub + key_code(slot & 15, d0);
-            if constexpr (E == 1) *p = (char)w;
-            if constexpr (E == 2) *reinterpret_cast<uint16_t *>(p) = (uint16_t)w;
-            if constexpr (E == 4) *reinterpret_cast<uint32_t *>(p) = w;
+                for (int e = 0; e < E; ++e) sub[value_code(slot & 15, d0 + e)] = (char)(w[e / 4] >> (8 * (e & 3)));
+            } else {
+                uint32_t *p = reinterpret_cast<uint32_t *>(sub + key_code(slot & 15, d0));
+#pragma unroll
+                for (int e = 0; e < E / 4; ++e) p[e] = w[e];
+            }
+            if ((lane & 15) == 0) scales[u] = scale;
         }
-        if (lane == 0) scales[u] = scale;
-        if (u + waves * (int)gridDim.y < units) vector(u + waves * gridDim.y, x);
+        const int next = u0 + 4 * waves * gridDim.y;
+        if (next < units) vector(min(next + quarter, units - 1), x);
     }
     // (a workgroup to a request: its waves have read the length)
     if (a.advance && threadIdx.x == 0) a.ctx_lens[r] = t + 1;
@@ -398,8 +412,8 @@ hipError_t launch_kv8_append(const AppendArgs &a, hipStream_t s)
 {
     if (a.batch == 0) return hipSuccess;
     // (where the call advances the lengths a request is one workgroup's: another may have yet to read them)
-    const int threads = a.advance ? kAdvanceThreads : kThreads, waves = threads / 64;
-    const dim3 grid((unsigned)a.batch, a.advance ? 1u : (unsigned)((2 * a.num_kv_heads + waves - 1) / waves)), block((unsigned)threads);
+    const int threads = a.advance ? std::min(kAdvanceThreads, (2 * a.num_kv_heads + 3) / 4 * 64) : kThreads, waves = threads / 64;
+    const dim3 grid((unsigned)a.batch, a.advance ? 1u : (unsigned)((2 * a.num_kv_heads + 4 * waves - 1) / (4 * waves))), block((unsigned)threads);
     if (a.head_dim == 64) hipLaunchKernelGGL(kv8_append<64>, grid, block, 0, s, a);
     else if (a.head_dim == 128) hipLaunchKernelGGL(kv8_append<128>, grid, block, 0, s, a);
     else if (a.head_dim == 256) hipLaunchKernelGGL(kv8_append<256>, grid, block, 0, s, a);
