@@ -102,6 +102,8 @@
  *           finite number
  *   So a block's scale grows with its tokens and begins anew with slot 0; a change of
  *   scale is exact but for codes of the smallest sizes (below 2^-6 of the new scale).
+ *   All appended tokens of a block are one request's, by one call at a time (its scales are
+ *   read and written); any number of requests may read it.
  *   A block's image in host memory has its scales with it.  part_tokens must be 0, and
  *   lamps_rope_append and lamps_rope_append_tokens refuse such a cache; all other calls
  *   take it.
@@ -263,8 +265,8 @@ int lamps_validate_args(lamps_ctx *ctx, int32_t batch, const int32_t *block_tabl
  * part_tokens == 0; the split ranges' partial results and their records
  * go to the library's own LAMPS_STATIC_SCRATCH_BYTES array on the current device
  * instead of a caller-provided workspace.  The call allocates nothing (no
- * hipMalloc / hipFree, no host heap) and enqueues one kernel or two on
- * compute_stream (hipStream_t as void*, NULL = the default stream) of the
+ * hipMalloc / hipFree, no host heap) and enqueues one kernel or two (LAMPS_E4M3: for
+ * every 256 requests) on compute_stream (hipStream_t as void*, NULL = the default stream) of the
  * current device.
  *   cfg           host; validated as by lamps_create (staging / copy fields are ignored);
  *                 part_tokens must be 0
@@ -274,7 +276,8 @@ int lamps_validate_args(lamps_ctx *ctx, int32_t batch, const int32_t *block_tabl
  * (head_dim + 2) floats for each wavefront resident on the chip -- must fit
  * 32 MiB of the array (on an MI355X: 4.3 MB for 32 heads on 32 kv heads of 128,
  * 8.5 MB for 32 on 8, 34 MB -- too much -- for 64 on 4); a geometry beyond that
- * is refused with LAMPS_ERR_RANGE and nothing is enqueued.
+ * is refused with LAMPS_ERR_RANGE and nothing is enqueued.  (LAMPS_E4M3: ranges are cut
+ * into no more parts than fit; no geometry is refused.)
  * All calls on one GPU share that GPU's array, which keeps the last call's
  * contents (nothing in it has to be cleared: no launch uses what it has not
  * written): calls that overlap on one GPU -- two streams, two threads -- race and
@@ -364,7 +367,8 @@ int lamps_kv_read_tokens(lamps_ctx *ctx, int32_t layer, int32_t n_req, int32_t t
  * bf16 before the second product), fp32 on the fp32 matrix instruction (fp32
  * weights); other geometries -- also pools whose blocks lie 4 GiB or more apart --
  * and any geometry when max_new_tokens < 0, run one wavefront per new token with
- * fp32 weights. */
+ * fp32 weights.  LAMPS_E4M3 is as bf16, a wavefront per token having its weights as pairs of
+ * bf16 (16 bits of fraction), and leaves no row unwritten for a bound that is too small. */
 int lamps_prefill_attn(lamps_ctx *ctx, int32_t layer, int32_t n_req, int32_t total_tokens,
                        int32_t max_new_tokens, const void *q, const int32_t *q_start,
                        const int32_t *block_table, const int32_t *ctx_lens, void *out);

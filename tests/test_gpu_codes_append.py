@@ -20,6 +20,7 @@ FORMS = [
     (8, 2, 256, 64, [[61, 90], [70, 1]]),
     (2, 1, 128, 256, [[300, 5], [30, 300]]),
     (40, 40, 128, 32, [[40, 7], [5, 5]]),
+    (3, 3, 64, 16, [[9, 20], [8, 1]]),
 ]
 # sizes of a call's numbers: as drawn; growing from call to call, so that scales move; shrinking; far apart within a vector
 SIZES = {"alike": lambda c: 1.0, "growing": lambda c: 7.0 ** c, "much larger": lambda c: 1e4 ** c, "shrinking": lambda c: 20.0 ** -c}
