@@ -215,9 +215,10 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
     constexpr int kCols = 16 * kCB, CG = kWaves / PS, NK = D / 32, NS = D / 16;   // columns of a wave; waves with columns of their own
     constexpr int SUBK = 16 * D * 2, VOFF = 2 * SUBK, STAGE = 4 * SUBK;   // bytes of a sub-tile of keys, where values begin, of a stage
     constexpr bool kHold = D <= 128;                     // operands of a stage are held in registers
-    __shared__ __align__(16) char lds[2 * PS * STAGE];
+    constexpr int RING = kHold && PS == 1 ? 4 : 2;       // rounds that there are buffers for
+    __shared__ __align__(16) char lds[RING * PS * STAGE];
     constexpr int SUBS = D == 256 ? 2 : 1, KINDS = D == 64 ? 1 : 2;   // of a thread's units: sub-tiles, keys and values
-    __shared__ uint32_t wild_at[2 * PS][kWaves * SUBS];
+    __shared__ uint32_t wild_at[RING * PS][kWaves * SUBS];
 
     const DecodeArgs &a = w.d;
     const int G = a.num_q_heads / a.num_kv_heads, TW = kCols / G, WT = CG * TW;
@@ -278,8 +279,7 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
             } else {
                 p = t + 16 * sub < see.end ? t + 16 * sub : t;
             }
-            // (an entry that names no block of the pool reads the last one: the rows are meaningless)
-            x.block[i] = min((uint32_t)table[p >> a.log2_block_size], last_block);
+            x.block[i] = (uint32_t)table[p >> a.log2_block_size];
             x.at[i] = (uint32_t)(p & in_block) * D;
         }
         return x;
@@ -291,7 +291,8 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
     const auto load = [&](const Places &x, Codes &y) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < SUBS; ++i) {
-            const uint64_t block = (uint64_t)x.block[i] * stride, off = block + x.at[i];
+            // (an entry that names no block of the pool reads the last one: the rows are meaningless.  Not looked at before it is used: nothing waits for it)
+            const uint64_t block = (uint64_t)min(x.block[i], last_block) * stride, off = block + x.at[i];
             y.scale[i] = __builtin_bit_cast(float2, *(scales_ptr)(uintptr_t)(sp + block));
             if constexpr (KINDS == 2) {
                 y.raw[i][0] = *reinterpret_cast<const uint4 *>(kp + off + u16);
@@ -348,12 +349,12 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
 
     if (lane == 0) {
 #pragma unroll
-        for (int i = 0; i < SUBS; ++i) for (int k = 0; k < 2 * PS; ++k) wild_at[k][kWaves * i + wv] = 0;
+        for (int i = 0; i < SUBS; ++i) for (int k = 0; k < RING * PS; ++k) wild_at[k][kWaves * i + wv] = 0;
     }
     // A round of the walk is PS stages, one for each of the waves that share columns.  Codes are asked for a round ahead of their conversion, the first in front of the
     // queries (two rounds ahead is no faster: 12 responses 84 us, 4 prompts of 4 096 1 008, either way).
     Places next[PS];
-    Codes codes[PS];
+    Codes codes[PS], early[RING == 4 ? 2 : 1][PS];
     const auto lookup_round = [&](int st) __attribute__((always_inline)) {
 #pragma unroll
         for (int k = 0; k < PS; ++k) next[k] = lookup(st + k);
@@ -370,6 +371,12 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
         lookup_round(st0);
         load_round(codes);
         lookup_round(st0 + PS);
+        if constexpr (RING == 4) {
+            load_round(early[0]);
+            lookup_round(st0 + 2 * PS);
+            load_round(early[1]);
+            lookup_round(st0 + 3 * PS);
+        }
     }
 
     // this lane's column in each block: (token, head), its position, its queries (of a negative scale: their negatives)
@@ -496,8 +503,10 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
     };
 
     // Operands of keys for the stage at hand are in registers where its iteration begins, those of values are asked for in front of its products
-    // (heads of 256: both where they are used, for want of registers).  Behind the softmax a barrier: everyone has what the stage's buffer held, and the other one is
-    // whole; the next keys are read, and the next stage but one is converted, while the matrix cores multiply values.
+    // (heads of 256: both where they are used, for want of registers).  Behind the softmax a barrier: everyone has what the stage's buffer held, and the next one is
+    // whole; the next keys are read, and a later stage is converted, while the matrix cores multiply values.  With four buffers a barrier in every second round does: the third round
+    // ahead is converted into the buffer that two rounds, and a barrier since, have left (two buffers and a barrier a round / so: 4 prompts of 4 096, 32 / 8 heads, 993 us and 970, 24 of 16 to
+    // 700 on 40 plain ones 115 and 111).
     bf16x8 kop[kHold ? NK : 1][2];
     uint4 vheld[kHold ? NS : 1];
     const char *mine = lds + lane * 16;                  // (unit qd * 16 + j)
@@ -512,7 +521,12 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
     };
     if (st0 < st1) {
         put_round(st0, 0, codes);
-        if constexpr (kHold) {
+        if constexpr (RING == 4) {
+            put_round(st0 + PS, 1, early[0]);
+            put_round(st0 + 2 * PS, 2, early[1]);
+            load_round(codes);
+            lookup_round(st0 + 4 * PS);
+        } else if constexpr (kHold) {
             load_round(codes);
             lookup_round(st0 + 2 * PS);
             put_round(st0 + PS, 1, codes);               // (past the last stage: the last one once more, which nobody reads)
@@ -527,7 +541,7 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
         __syncthreads();
         if (st0 < st1) read_k(mine + ps * STAGE);
     }
-    // The round from stage rd on, whose buffer is `cur`; x: the codes that it converts, and then asks for others.
+    // The round from stage rd on, whose buffer is `cur`; past the last stage the last one is converted once more, which nobody reads.
     const auto round = [&](int rd, auto parity) __attribute__((always_inline)) {
         constexpr int cur = parity;
         if constexpr (!kHold) {
@@ -578,11 +592,12 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
             }
         }
         if constexpr (kHold) {
-            __syncthreads();
-            read_k(mine + ((cur ^ 1) * PS + ps) * STAGE);
-            put_round(rd + 2 * PS, cur, codes);
+            if (RING == 2 || (cur & 1)) __syncthreads();
+            read_k(mine + ((cur + 1) % RING * PS + ps) * STAGE);
+            constexpr int far = RING == 4 ? 3 : 2;
+            put_round(rd + far * PS, (cur + far) % RING, codes);
             load_round(codes);
-            lookup_round(rd + 4 * PS);
+            lookup_round(rd + (far + 2) * PS);
         }
         if (!live) return;
 #pragma unroll
@@ -596,9 +611,13 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
         }
     };
     // (heads of 256: the first round is converted by itself, and the second's codes come first)
-    for (int rd = st0; rd < st1; rd += 2 * PS) {
+    for (int rd = st0; rd < st1; rd += RING * PS) {
         round(rd, std::integral_constant<int, 0>{});
         if (rd + PS < st1) round(rd + PS, std::integral_constant<int, 1>{});
+        if constexpr (RING == 4) {
+            if (rd + 2 * PS < st1) round(rd + 2 * PS, std::integral_constant<int, 2>{});
+            if (rd + 3 * PS < st1) round(rd + 3 * PS, std::integral_constant<int, 3>{});
+        }
     }
     // (the last products are there before what adds them up or stores them: see window_tiles.h)
     asm volatile("s_nop 7" ::: "memory");
