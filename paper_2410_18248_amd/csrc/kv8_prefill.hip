@@ -52,8 +52,9 @@ __device__ __forceinline__ float wave_sum(float x)
 }
 
 // How a launch that cuts divides its work, by every wave for itself, K consecutive requests per lane.
-template <int K>
+template <int K, bool WINDOW>
 struct TilePlan {
+    bool any;                                            // request's tiles may be cut
     int first[K], count[K], ctx[K], tiles[K], runs[K];   // first row, new tokens, length; tiles, and parts of each (1: not cut)
 
     __device__ __forceinline__ TilePlan(const WindowArgs &w, const Tiling &c, int WT)
@@ -77,7 +78,8 @@ struct TilePlan {
             const int rows = on ? min(count[k], w.total_tokens - first[k]) : 0;
             tiles[k] = max(0, (rows + WT - 1) / WT);
             const int p = ctx[k] - count[k] + rows;      // (the last tile's end, and what its first token sees)
-            stages[k] = tiles[k] > 0 ? Sight<32>(p, max(0, p - min(rows, WT) - w.window + 1), w.sinks, std::true_type{}).units : 0;
+            if constexpr (WINDOW) stages[k] = tiles[k] > 0 ? Sight<32>(p, max(0, p - min(rows, WT) - w.window + 1), w.sinks, std::true_type{}).units : 0;
+            else stages[k] = tiles[k] > 0 ? (p + 31) / 32 : 0;
             work += (float)stages[k] * (float)tiles[k];
         }
         // an even share (the sum is off by a few times 2^-24)
@@ -87,6 +89,13 @@ struct TilePlan {
         // more of them than places (12 responses of 4 to 64 tokens on 300 to
         // 30 000, 32 / 8 heads: 853 parts of an even share and up to half as much again, 114 us; 504 so, 84; the line of all tiles in even shares, the ends of tiles in the middle of
         // one, 90 to 96: two workgroups of a CU share what they wait for, and a tile's beginning and end cost what 8 stages do).
+        any = c.later != 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            runs[k] = 1;
+            any |= __any(stages[k] > size + size / 2) != 0;
+        }
+        if (!any) return;                                // (most launches of many tiles)
         for (int tries = c.later ? kTries : 0;; --tries) {
             const int worth = c.later ? size : size + size / 2;
             int sum = 0;
@@ -132,11 +141,24 @@ __device__ __forceinline__ bool find_request(const int (&mine)[K], int &at, int 
     return true;
 }
 // The piece'th of all parts, cut requests' first, of each request the longest tile first.
-template <int K>
+template <int K, bool WINDOW>
 __device__ __forceinline__ bool find_tile(const WindowArgs &w, const Tiling &c, int WT, int piece, TilePiece &x)
 {
-    const TilePlan<K> plan(w, c, WT);
+    const TilePlan<K, WINDOW> plan(w, c, WT);
     int cuts[K], others[K], sum = 0, at = piece, k_of = 0, l_of = 0;
+    if (!plan.any) {
+        if (!find_request<K>(plan.tiles, at, k_of, l_of)) return false;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (k == k_of) {
+                plan.take(k, l_of, x);
+                x.runs = 1;
+                x.at = 0;
+                x.item = piece;
+                x.tile = __builtin_amdgcn_readlane(plan.tiles[k], l_of) - 1 - at;
+            }
+        return true;
+    }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         cuts[k] = plan.cut(k) ? plan.tiles[k] * plan.runs[k] : 0;
@@ -158,10 +180,10 @@ __device__ __forceinline__ bool find_tile(const WindowArgs &w, const Tiling &c, 
     return true;
 }
 // The nth tile that is cut: its request, and the number of its first part.
-template <int K>
+template <int K, bool WINDOW>
 __device__ __forceinline__ bool find_cut_tile(const WindowArgs &w, const Tiling &c, int WT, int nth, TilePiece &x)
 {
-    const TilePlan<K> plan(w, c, WT);
+    const TilePlan<K, WINDOW> plan(w, c, WT);
     int cuts[K], own = 0, at = nth, k_of = 0, l_of = 0;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -226,7 +248,7 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
     // (heads next to each other: with 8 of them and more all tiles of one go to one XCD, whose L2 has its keys and values)
     const int piece = __builtin_amdgcn_readfirstlane((int)((unsigned)blockIdx.x / (unsigned)a.num_kv_heads));
     at.g = blockIdx.x - piece * a.num_kv_heads;
-    if (c.places == 0 ? !find_whole_tile(w, WT, piece, at) : a.batch <= 64 ? !find_tile<1>(w, c, WT, piece, at) : !find_tile<4>(w, c, WT, piece, at)) return;
+    if (c.places == 0 ? !find_whole_tile(w, WT, piece, at) : a.batch <= 64 ? !find_tile<1, WINDOW>(w, c, WT, piece, at) : !find_tile<4, WINDOW>(w, c, WT, piece, at)) return;
     const int g = at.g, first = at.first, base_pos = at.ctx - at.n_new, n_new = min(at.n_new, w.total_tokens - first);
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 15, qd = lane >> 4;
 
@@ -743,7 +765,7 @@ __global__ __launch_bounds__(kThreads) void kv8_join(const WindowArgs w, const T
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 15, qd = lane >> 4;
     const int nth = __builtin_amdgcn_readfirstlane((int)((unsigned)blockIdx.x / (unsigned)a.num_kv_heads)), g = blockIdx.x - nth * a.num_kv_heads, block = blockIdx.y;
     TilePiece at;
-    if (a.batch <= 64 ? !find_cut_tile<1>(w, c, WT, nth, at) : !find_cut_tile<4>(w, c, WT, nth, at)) return;
+    if (a.batch <= 64 ? !find_cut_tile<1, WINDOW>(w, c, WT, nth, at) : !find_cut_tile<4, WINDOW>(w, c, WT, nth, at)) return;
     const int base_pos = at.ctx - at.n_new, n_new = min(at.n_new, w.total_tokens - at.first), wave_tok = at.tile * WT + block / kCB * TW;
     if (wave_tok >= n_new) return;                       // (the wave had no tokens and has left nothing)
     const int p_first = base_pos + at.tile * WT, p_last = base_pos + min(n_new, (at.tile + 1) * WT) - 1;
@@ -881,9 +903,11 @@ hipError_t launch(const WindowArgs &w, hipStream_t s)
         // (of 64 columns two workgroups fit a CU, of 128 one: 4 prompts of 1 024, 16 / 4 heads, 88 us and 119)
         return G <= 16 ? launch_tiles<D, 1, 1>(w, s) : launch_tiles<D, 2, 1>(w, s);
     } else {
-        // (few columns: four waves on 64 of them and two stages at a time.  12 requests of 4 to 64 tokens on 300 to 3 000, 32 plain heads, by 128 and by 64 columns, us: 70
-        // and 46; 16 of 512, 32 / 8 heads: 75 and 109; the responses of above 85 and 84)
-        const bool narrow = (long long)w.max_new_tokens * G <= 256;
+        // Four waves on 64 columns and two stages at a time where a request has no more columns, or few more and the launch few tiles; else each 32 of 128.  By 64 / 128, us, all
+        // on 3 000 cached: 64 requests of 16 tokens, 32 / 8 heads, 85 / 99, of 24 142 / 106, of 64 267 / 218; 16 of 48 69 / 84; 4 of 192 on 40 plain heads 72 / 106, 64 of 32 368 / 414, of
+        // 128 725 / 598.  (Without contexts by 128 always, 64 of 16 10.2 and 13.3; but the host does not know.)  12 of 4 to 64 on 300 to 30 000 80 / 85.
+        const long long columns = (long long)w.max_new_tokens * G, tiles = (long long)w.total_tokens * G / 64 + a.batch;
+        const bool narrow = columns <= 64 || (columns <= 256 && tiles * a.num_kv_heads <= 1024);
         return narrow ? launch_tiles<D, 2, 2>(w, s) : launch_tiles<D, 2, 1>(w, s);
     }
 }
