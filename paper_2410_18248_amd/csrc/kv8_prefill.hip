@@ -29,6 +29,7 @@ struct Tiling {
 };
 constexpr int kMostRequests = 256;                       // of a launch that cuts
 constexpr int kLeastStages = 8;                          // of a part
+constexpr int kWorth = 16;                               // by which a tile is longer, where it is worth a sum of parts
 constexpr int kTries = 12;
 
 // What a workgroup takes.
@@ -85,19 +86,22 @@ struct TilePlan {
         // an even share (the sum is off by a few times 2^-24)
         const float even = wave_sum(work) * (float)a.num_kv_heads / (float)c.places * 1.00001f + 1.0f;
         int size = max(kLeastStages, even < (float)(1 << 26) ? (int)even : 1 << 26);
+        // Parts cost their beginnings and a sum: nothing is cut where no tile is much longer than an even share.  By a size of 1.5 shares (few tiles: one) and more / so, us, 32 / 8 heads:
+        // one prompt of 1 000 37 / 26, 4 of 400 27 / 19, 12 of 30 tokens on 500 22 / 16; 16 / 4 heads of 256, 1 000 39 / 33.  Few tiles by 2 shares and 32 more: 4 of 128 on 2 000 53 / 40.
         // Where the parts are added up by a second launch they are of about one size, and the chip holds all of them at once: from an even share their size goes up until there are no
-        // more of them than places (12 responses of 4 to 64 tokens on 300 to
-        // 30 000, 32 / 8 heads: 853 parts of an even share and up to half as much again, 114 us; 504 so, 84; the line of all tiles in even shares, the ends of tiles in the middle of
-        // one, 90 to 96: two workgroups of a CU share what they wait for, and a tile's beginning and end cost what 8 stages do).
-        any = c.later != 0;
+        // more of them than places (12 responses of 4 to 64 tokens on 300 to 30 000, 32 / 8 heads: 853 parts of an even share and up to half as much again, 114 us; 504 so, 84; the
+        // line of all tiles in even shares, the ends of tiles in the middle of one, 90 to 96: two workgroups of a CU share what they wait for, and a tile's beginning and end cost what 8
+        // stages do).
+        const int least = c.later ? 2 * size + kWorth : max(size + size / 2, kWorth + 4);
+        any = false;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             runs[k] = 1;
-            any |= __any(stages[k] > size + size / 2) != 0;
+            any |= __any(stages[k] > least) != 0;
         }
         if (!any) return;                                // (most launches of many tiles)
         for (int tries = c.later ? kTries : 0;; --tries) {
-            const int worth = c.later ? size : size + size / 2;
+            const int worth = c.later ? size : least;
             int sum = 0;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
@@ -868,9 +872,8 @@ hipError_t launch_tiles(const WindowArgs &w, hipStream_t s)
         c.places = (int)std::min(512LL, room / 2 - 1);
         if (c.places < 1) c.places = 0;
         c.items = (int)std::min(room, 1024LL);
-        // Few tiles, which are cut where contexts are long (a row of fewer stages than one and a half parts cannot be).  The last part to arrive adds up: the responses 109 us, 16 tokens
-        // on 8 000 49; a second launch: 84 and 21.
-        c.later = c.places > 0 && tiles * heads < 512 && (long long)a.max_blocks * a.block_size > 32 * kLeastStages * 3 / 2;
+        // Few tiles, where a table row holds contexts that are cut.  The last part to arrive adds up: the responses 109 us, 16 tokens on 8 000 49; a second launch: 84 and 21.
+        c.later = c.places > 0 && tiles * heads < 512 && (long long)a.max_blocks * a.block_size > 32 * (2 * kLeastStages + kWorth);
     }
     const long long grid = (tiles * heads + (c.places > 0 ? 2LL * c.places : 0) + heads - 1) / heads * heads;
     if (grid > 0x7fffffffLL) return hipErrorInvalidValue;

@@ -28,6 +28,10 @@ FORMS = [
     (2, 1, 128, 64, [(9000, 70)]),
     (32, 2, 128, 16, [(1100, 1100), (1500, 1000), (40, 40)]),     # many tiles
     (16, 16, 128, 32, [(2100, 2100), (2600, 2050), (1, 1)]),
+    (8, 2, 64, 64, [(928, 928)]),                                # parts that the last of them adds up: short rows
+    (16, 4, 256, 16, [(1000, 1000), (7, 3)]),
+    (32, 32, 64, 16, [(5000, 5)] + [(30, 30)] * 16),             # and one long context beside many tiles
+    (8, 2, 128, 16, [(3000, 70), (800, 70)]),
 ]
 
 
