@@ -28,10 +28,14 @@ struct Split {
 // What a workgroup takes: units u0 .. u1 - 1 of a range, one of `runs` parts of it (the at'th; `first`: the item of the first).
 struct Piece {
     int r, hc, C, u0, u1, runs, at, first;
+    bool single;                                         // a range of the wave's own
 };
 constexpr int kLeastUnits = 2 * kWaves;                  // of a part
 constexpr int kMostRequests = 256;                       // of a launch
 constexpr int kMostUnits = 1 << 26;
+// So many ranges of no more units go to a wave each, which needs no other (a workgroup / a wave, us: 256 requests of 60 on 40 plain heads 62.5 / 41.5, of 120 77.8 / 63.9, of 60 on
+// 32 / 8 heads 15.6 / 10.6; 202 of 60 on 16 plain heads of 256 65.7 / 41.1): the workgroups that are too many leave at once.
+constexpr int kShortUnits = 4, kManyRanges = 1024;
 
 __device__ __forceinline__ int divided(int a, int b) { return (int)((unsigned)a / (unsigned)b); }
 
@@ -99,8 +103,10 @@ __device__ __forceinline__ bool find_piece(const WindowArgs &w, const Split &c, 
     const int lane = threadIdx.x & 63, HC = a.num_kv_heads * a.passes;
     const Plan<K> plan(w, c);
     const auto &[n, C, np, own, upto, cuts, whole, longest, worth] = plan;
+    it.single = longest <= kShortUnits && whole * HC >= kManyRanges;
+    if (it.single) item = item * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (item >= cuts + whole * HC) return false;
-    if (item < cuts) {
+    if (item < cuts) {                                   // (none, where `single`: a part has kLeastUnits and more)
         int at = divided(item, HC);
         it.hc = item - at * HC;
         const int l = __popcll(__ballot(upto <= at));
@@ -191,12 +197,20 @@ __global__ __launch_bounds__(kThreads, D >= 256 ? 1 : 2) void kv8_decode(const W
     Piece it;
     if (a.batch <= 64 ? !find_piece<1>(w, c, blockIdx.x, it) : !find_piece<4>(w, c, blockIdx.x, it)) return;
     const Sight<32> see(it.C, w.window, w.sinks);
-    const int u1 = min(it.u1, see.units), n = max(u1 - it.u0, 0), each = (n + kWaves - 1) / kWaves, from = min(n, wv * each);
-    R::run(a, it.r, (size_t)it.r, it.hc / a.passes, it.hc * GH, GH, see, it.u0 + from, it.u0 + min(n, from + each),
-           [&](int h, int d, float M, float L, const auto &A) { store_partial(states + (size_t)(wv * GH + h) * (D + 2), D, d, M, L, A); });
-    __syncthreads();
+    const int u1 = min(it.u1, see.units), n = max(u1 - it.u0, 0), each = it.single ? n : (n + kWaves - 1) / kWaves, from = it.single ? 0 : min(n, wv * each);
     const bool wide = ((uintptr_t)a.out & 3) == 0;
     const size_t slot = (size_t)GH * (D + 2), row = ((size_t)it.r * a.num_q_heads + it.hc * GH) * D;
+    R::run(a, it.r, (size_t)it.r, it.hc / a.passes, it.hc * GH, GH, see, it.u0 + from, it.u0 + min(n, from + each), [&](int h, int d, float M, float L, const auto &A) {
+        if (it.single) {                                 // uniform
+            const float inv = see.units == 0 ? 0.0f : 1.0f / L;
+            put_pair(a.out, row + h * D + d, wide, A[0] * inv, A[1] * inv);
+            put_pair(a.out, row + h * D + d + 2, wide, A[2] * inv, A[3] * inv);
+        } else {
+            store_partial(states + (size_t)(wv * GH + h) * (D + 2), D, d, M, L, A);
+        }
+    });
+    if (it.single) return;
+    __syncthreads();
     // the waves' states added up: pair i of outputs, of head h from dim d on
     const auto add_up = [&](auto out) {
         for (int i = 2 * (64 * wv + lane); i < GH * D; i += 128 * kWaves) {
@@ -343,11 +357,12 @@ hipError_t launch(WindowArgs w, hipStream_t s)
     const size_t room = std::min((size_t)decode_max_shares(a.heads_per_pass, D) * per_share, (size_t)LAMPS_STATIC_SCRATCH_BYTES - ((size_t)1 << 20));
     // Few ranges, all of which may be cut: parts for one workgroup to a CU, and a second launch for the sums, whose workgroups share the parts of a range: by the last of them to
     // arrive, which is alone with them, / so, us: one request of 30 000 on 32 / 8 heads 19.6 / 17.0, 60 000 on 32 / 4 28.0 / 18.1, 8 000 14.1 / 10.9, 1 999 10.0 / 9.5;
+    // (no gain where table rows hold 1 024 positions at most: 100 6.1 / 7.3, 700 8.3 / 8.6; all by the last / by a second launch)
     // 16 of 2 000 15.2 / 16.6, 200 of 100 to 4 000 on 8 / 2 heads of 64 14.8 / 21.1.  Otherwise 256 places, or 512 where there are hundreds of ranges (256 / 512 / 1 024: 16 of 2 000
     // 15.2 / 16.1 / 22.6, 32 of 100 to 4 000 on 16 / 4 heads of 256 20.4 / 25.0 / 24.9; those 200 14.7 / 13.5 / 15.7, 230 of 32 to 8 192 on 32 / 8 heads 104.5 / 97.4 /
     // 100.0).
     const long long ranges = (long long)a.batch * HC;
-    const bool later = ranges < 128;
+    const bool later = ranges < 128 && (long long)a.max_blocks * a.block_size > 1024;
     int log2_places = ranges < 384 ? 8 : 9;
     while (log2_places > 0 && ((size_t)2 << log2_places) * (state + 8) > room) --log2_places;
     if (((size_t)2 << log2_places) * (state + 8) > std::min(room, a.partial_capacity)) return hipErrorInvalidValue;

@@ -34,6 +34,11 @@ FORMS = [
     (17, 1, 128, 16, [80, 5]),                                 # 17 passes of one
     (8, 2, 128, 16, [5000, 30, 900, 1, 2500, 64]),             # cut
     (2, 1, 64, 32, [9000]),
+    (8, 8, 64, 16, [(37 * i) % 129 for i in range(150)]),        # many short ranges: a wave each
+    (40, 40, 128, 32, [(17 * i) % 97 for i in range(30)]),
+    (32, 8, 128, 16, [(29 * i) % 129 for i in range(131)]),
+    (16, 16, 256, 16, [(53 * i) % 127 for i in range(67)]),
+    (96, 3, 64, 16, [5] * 200 + [128] * 70),                     # the same in two passes, and a second launch for 14 requests
 ]
 
 
