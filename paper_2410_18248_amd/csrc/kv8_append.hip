@@ -168,7 +168,8 @@ __device__ __forceinline__ bool block_at(const CodesArgs &a, int w, int log2, Bl
 // One workgroup per (block that holds new tokens, kv head), which alone decides its two scales and writes it.  A unit is 16 bytes of codes: of
 // keys 16 dims of a slot; of values, for four slots, dims j + 16 s of a group of 64, which four lanes, one for each s, load four dims j at a time of
 // and transpose among themselves.  The numbers are loaded for the largest of them, kept (HOLD units to a thread, where a block has no more; else they are loaded
-// again, out of L2) and rounded.
+// again, out of L2) and rounded.  Bound by memory: 4 prompts of 4 096 tokens, 8 heads of 128, 101 MB, 21.9 to 23.7 us, 4.3 to 4.6 TB/s; 12 responses of 4 to 64 tokens 4.8, the launch and the
+// round trips.
 template <int D, int HOLD>
 __global__ __launch_bounds__(kThreads) void kv8_append_tokens(const CodesArgs a)
 {
@@ -320,7 +321,7 @@ __global__ __launch_bounds__(kThreads) void kv8_append_tokens(const CodesArgs a)
 
 // ---------------------------------------------------------------- reading back
 
-// One workgroup per (request, 16 positions of which some are asked for, kv head).
+// One workgroup per (request, 16 positions of which some are asked for, kv head).  Bound by memory: 383 MB of 40 heads of 128, two thirds of them written, 85 us, 4.5 TB/s.
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv8_read_tokens(const CodesArgs a, uint16_t *k_out, uint16_t *v_out)
 {
