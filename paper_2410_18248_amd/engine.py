@@ -86,7 +86,8 @@ class LiveEngine:
         if rope is not None and cfg.dtype == P.LAMPS_E4M3:
             raise ValueError("rotary appends do not go into a cache of 8 bits")
         self.tdtype = torch.float32 if cfg.dtype == P.LAMPS_F32 else torch.bfloat16     # of the rows
-        self.k_pool, self.v_pool = (torch.zeros(P.lamps_pool_bytes(cfg), dtype=torch.uint8, device=self.dev) for _ in range(2))
+        held = torch.uint8 if cfg.dtype == P.LAMPS_E4M3 else self.tdtype     # what the pools hold (codes and scales: bytes)
+        self.k_pool, self.v_pool = (torch.zeros(P.lamps_pool_bytes(cfg) // held.itemsize, dtype=held, device=self.dev) for _ in range(2))
         self.ws = torch.empty(P.lamps_workspace_bytes(cfg), dtype=torch.uint8, device=self.dev)
         self.cs, self.so, self.si = (torch.cuda.Stream(self.dev) for _ in range(3))
         torch.cuda.synchronize()
