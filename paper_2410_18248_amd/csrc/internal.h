@@ -120,6 +120,8 @@ hipError_t launch_prefill_window(const WindowArgs &a, hipStream_t stream);
 constexpr int32_t kEverything = 1 << 30;     // (no row has more positions)
 hipError_t launch_kv8_decode(const WindowArgs &a, hipStream_t stream);
 hipError_t launch_kv8_prefill(const WindowArgs &a, hipStream_t stream);
+// Bytes behind DecodeArgs::partials that hold as many parts of tiles as launch_kv8_prefill cuts a launch into: in less it cuts into fewer.
+size_t kv8_parts_bytes(int head_dim, int group);
 
 struct RopeArgs {
     const void *q, *k_new, *v_new;   // rows of [H or H_kv][D], the strides apart

@@ -32,6 +32,7 @@ struct Tiling {
     int later;                                           // parts are added up by a second launch
 };
 constexpr int kMostRequests = 256;                       // of a launch that cuts
+constexpr int kMostPlaces = 512;                         // workgroups that the chip holds at once
 constexpr int kLeastStages = 8;                          // of a part
 constexpr int kWorth = 16;                               // by which a tile is longer, where it is worth a sum of parts
 constexpr int kTries = 12;
@@ -871,11 +872,10 @@ hipError_t launch_tiles(const WindowArgs &w, hipStream_t s)
     const long long tiles = (long long)w.total_tokens / WT + a.batch, heads = a.num_kv_heads;
     Tiling c = {0, 0, 0};
     if (a.batch <= kMostRequests) {
-        // Parts are no more than twice the places (a range's n / size + 1, where n is more than size); two workgroups fit a CU.
+        // Parts are fewer than twice the places (a range's n / size + 1, where n is more than size, which is more than an even share); two workgroups fit a CU.
         const long long state = (long long)tile_state(D, CG * 16 * kCB) * (long long)sizeof(float), room = (long long)a.partial_capacity / (state + 8);
-        c.places = (int)std::min(512LL, room / 2 - 1);
-        if (c.places < 1) c.places = 0;
-        c.items = (int)std::min(room, 1024LL);
+        c.places = (int)std::min((long long)kMostPlaces, room / 2);
+        c.items = (int)std::min(room, 2LL * kMostPlaces);
         // Few tiles, where a table row holds contexts that are cut.  The last part to arrive adds up: the responses 109 us, 16 tokens on 8 000 49; a second launch: 84 and 21.
         c.later = c.places > 0 && tiles * heads < 512 && (long long)a.max_blocks * a.block_size > 32 * (2 * kLeastStages + kWorth);
     }
@@ -920,6 +920,12 @@ hipError_t launch(const WindowArgs &w, hipStream_t s)
 }
 
 }  // namespace
+
+size_t kv8_parts_bytes(int head_dim, int group)
+{
+    if (group > 32) return 0;                            // (a wavefront per token)
+    return 2 * kMostPlaces * (tile_state(head_dim, head_dim >= 256 && group <= 16 ? 64 : 128) * sizeof(float) + 8);
+}
 
 hipError_t launch_kv8_prefill(const WindowArgs &w, hipStream_t stream)
 {

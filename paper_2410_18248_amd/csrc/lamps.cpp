@@ -84,6 +84,8 @@ const char *derive(const lamps_config *c, Derived *d)
     } else {
         d->max_parts = 0;
         d->partial_bytes = (size_t)lamps::decode_max_shares(gh, c->head_dim) * 2 * gh * (c->head_dim + 2) * 4;
+        // (of 8 bits: the parts of tiles of many new tokens are a tile's columns each, however few heads a pass of decode has)
+        if (c->dtype == LAMPS_E4M3) d->partial_bytes = std::max(d->partial_bytes, lamps::kv8_parts_bytes(c->head_dim, group));
     }
     d->prefix_bytes = (size_t)(lamps::decode_max_shares(gh, c->head_dim) + 1) * 16;   // share_info
     if (c->staging_bytes < 0) return "staging_bytes is negative";
