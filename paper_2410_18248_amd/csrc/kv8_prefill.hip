@@ -19,6 +19,7 @@
 #include "handover.h"
 #include "internal.h"
 #include "kv8.h"
+#include "kv8_cut.h"
 #include "requests.h"
 #include "tile_parts.h"
 #include "kv8_decode.h"
@@ -28,14 +29,10 @@ namespace {
 
 struct Tiling {
     int items;                                           // parts that there is room for
-    int places;                                          // workgroups that all work is dealt to evenly where requests are cut; 0: none is
+    int log2_places;                                     // 2^it: workgroups that all work is dealt to evenly where requests are cut; -1: none is
     int later;                                           // parts are added up by a second launch
 };
 constexpr int kMostRequests = 256;                       // of a launch that cuts
-constexpr int kMostPlaces = 512;                         // workgroups that the chip holds at once
-constexpr int kLeastStages = 8;                          // of a part
-constexpr int kWorth = 16;                               // by which a tile is longer, where it is worth a sum of parts
-constexpr int kTries = 12;
 
 // What a workgroup takes.
 struct TilePiece {
@@ -43,21 +40,14 @@ struct TilePiece {
     int runs, at, item;                                  // part `at` of up to `runs`; the item of the first
 };
 
-// Sum over the lanes of a wave, in all of them.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ float shifted(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, ROWS, 0xF, false)); }
-__device__ __forceinline__ float wave_sum(float x)
+// Sum of whole numbers below 2^48 over the lanes of a wave, in all of them.
+__device__ __forceinline__ uint64_t wave_sum(uint64_t x)
 {
-    x += shifted<0x111, 0xF>(x);                         // as wave_scan
-    x += shifted<0x112, 0xF>(x);
-    x += shifted<0x114, 0xF>(x);
-    x += shifted<0x118, 0xF>(x);
-    x += shifted<0x142, 0xA>(x);
-    x += shifted<0x143, 0xC>(x);
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+    const int low = wave_scan((int)(x & 0xFFFFFF)), high = wave_scan((int)(x >> 24));
+    return ((uint64_t)(unsigned)__builtin_amdgcn_readlane(high, 63) << 24) + (unsigned)__builtin_amdgcn_readlane(low, 63);
 }
 
-// How a launch that cuts divides its work, by every wave for itself, K consecutive requests per lane.
+// How a launch that cuts divides its work (kv8_cut.h), by every wave for itself, K consecutive requests per lane.
 template <int K, bool WINDOW>
 struct TilePlan {
     bool any;                                            // request's tiles may be cut
@@ -68,7 +58,7 @@ struct TilePlan {
         const DecodeArgs &a = w.d;
         const int lane = threadIdx.x & 63;
         int stages[K];
-        float work = 0.0f;
+        uint64_t work = 0;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int i = min(K * lane + k, a.batch - 1);
@@ -86,35 +76,31 @@ struct TilePlan {
             const int p = ctx[k] - count[k] + rows;      // (the last tile's end, and what its first token sees)
             if constexpr (WINDOW) stages[k] = tiles[k] > 0 ? Sight<32>(p, max(0, p - min(rows, WT) - w.window + 1), w.sinks, std::true_type{}).units : 0;
             else stages[k] = tiles[k] > 0 ? (p + 31) / 32 : 0;
-            work += (float)stages[k] * (float)tiles[k];
+            work += cut8::work_of(stages[k], tiles[k]);
         }
-        // an even share (the sum is off by a few times 2^-24)
-        const float even = wave_sum(work) * (float)a.num_kv_heads / (float)c.places * 1.00001f + 1.0f;
-        int size = max(kLeastStages, even < (float)(1 << 26) ? (int)even : 1 << 26);
-        // Parts cost their beginnings and a sum: nothing is cut where no tile is much longer than an even share.  By a size of 1.5 shares (few tiles: one) and more / so, us, 32 / 8 heads:
-        // one prompt of 1 000 37 / 26, 4 of 400 27 / 19, 12 of 30 tokens on 500 22 / 16; 16 / 4 heads of 256, 1 000 39 / 33.  Few tiles by 2 shares and 32 more: 4 of 128 on 2 000 53 / 40.
-        // Where the parts are added up by a second launch they are of about one size, and the chip holds all of them at once: from an even share their size goes up until there are no
-        // more of them than places (12 responses of 4 to 64 tokens on 300 to 30 000, 32 / 8 heads: 853 parts of an even share and up to half as much again, 114 us; 504 so, 84; the
-        // line of all tiles in even shares, the ends of tiles in the middle of one, 90 to 96: two workgroups of a CU share what they wait for, and a tile's beginning and end cost what 8
-        // stages do).
-        const int least = c.later ? 2 * size + kWorth : max(size + size / 2, kWorth + 4);
         any = false;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             runs[k] = 1;
-            any |= __any(stages[k] > least) != 0;
+            any |= __any(stages[k] > cut8::least_cut(cut8::kLeastStages, c.later)) != 0;
         }
+        if (!any) return;                                // (short walks: whatever the share is)
+        int size = cut8::first_size(wave_sum(work), a.num_kv_heads, c.log2_places);
+        const int least = cut8::least_cut(size, c.later);
+        any = false;
+#pragma unroll
+        for (int k = 0; k < K; ++k) any |= __any(stages[k] > least) != 0;
         if (!any) return;                                // (most launches of many tiles)
-        for (int tries = c.later ? kTries : 0;; --tries) {
+        for (int tries = c.later ? cut8::kTries : 0;; --tries) {
             const int worth = c.later ? size : least;
             int sum = 0;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                runs[k] = stages[k] > worth ? (int)((unsigned)(stages[k] + size - 1) / (unsigned)size) : 1;
+                runs[k] = cut8::runs_of(stages[k], size, worth);
                 sum += tiles[k] * runs[k];
             }
-            if (tries == 0 || __builtin_amdgcn_readlane(wave_scan(sum), 63) * a.num_kv_heads <= c.places) break;
-            size += size / 16 + 1;
+            if (tries == 0 || __builtin_amdgcn_readlane(wave_scan(sum), 63) * a.num_kv_heads <= 1 << c.log2_places) break;
+            size = cut8::next_size(size);
         }
     }
     __device__ __forceinline__ bool cut(int k) const { return runs[k] > 1; }
@@ -213,14 +199,6 @@ __device__ __forceinline__ bool find_cut_tile(const WindowArgs &w, const Tiling 
     }
     return true;
 }
-// Stages of each part of a tile of `units`, and parts that there are then: one of earlier tokens may have fewer stages than the request's last one, by which
-// the parts are counted.
-__device__ __forceinline__ int2 parts_of(int units, int runs)
-{
-    const int want = max(1, min(runs, units / (kLeastStages / 2))), each = (int)((unsigned)(units + want - 1) / (unsigned)want);
-    return make_int2(each, (int)((unsigned)(units + each - 1) / (unsigned)each));
-}
-
 // Without: any number of requests, none cut.
 __device__ __forceinline__ bool find_whole_tile(const WindowArgs &w, int WT, int piece, TilePiece &x)
 {
@@ -257,7 +235,7 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
     // (heads next to each other: with 8 of them and more all tiles of one go to one XCD, whose L2 has its keys and values)
     const int piece = __builtin_amdgcn_readfirstlane((int)((unsigned)blockIdx.x / (unsigned)a.num_kv_heads));
     at.g = blockIdx.x - piece * a.num_kv_heads;
-    if (c.places == 0 ? !find_whole_tile(w, WT, piece, at) : a.batch <= 64 ? !find_tile<1, WINDOW>(w, c, WT, piece, at) : !find_tile<4, WINDOW>(w, c, WT, piece, at)) return;
+    if (c.log2_places < 0 ? !find_whole_tile(w, WT, piece, at) : a.batch <= 64 ? !find_tile<1, WINDOW>(w, c, WT, piece, at) : !find_tile<4, WINDOW>(w, c, WT, piece, at)) return;
     const int g = at.g, first = at.first, base_pos = at.ctx - at.n_new, n_new = min(at.n_new, w.total_tokens - first);
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 15, qd = lane >> 4;
 
@@ -267,11 +245,11 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
     const auto position = [&](int st) { return WINDOW ? see.at(st) : st * 32; };
     int st0 = 0, st1 = see.units, runs = 1;
     if (at.runs > 1) {
-        const int2 parts = parts_of(see.units, at.runs);
-        runs = parts.y;
+        const cut8::Parts parts = cut8::parts_of(see.units, at.runs);
+        runs = parts.count;
         if (at.at >= runs) return;
-        st0 = at.at * parts.x;
-        st1 = min(see.units, st0 + parts.x);
+        st0 = at.at * parts.each;
+        st1 = min(see.units, st0 + parts.each);
     }
     st0 = __builtin_amdgcn_readfirstlane(st0);
     st1 = __builtin_amdgcn_readfirstlane(st1);
@@ -779,7 +757,7 @@ __global__ __launch_bounds__(kThreads) void kv8_join(const WindowArgs w, const T
     if (wave_tok >= n_new) return;                       // (the wave had no tokens and has left nothing)
     const int p_first = base_pos + at.tile * WT, p_last = base_pos + min(n_new, (at.tile + 1) * WT) - 1;
     const Sight<32> see(p_last + 1, WINDOW ? max(0, p_first - w.window + 1) : 0, WINDOW ? w.sinks : 0, std::true_type{});
-    const int runs = parts_of(see.units, at.runs).y;
+    const int runs = cut8::parts_of(see.units, at.runs).count;
     if (runs == 1) return;                               // (written already)
     constexpr size_t state = tile_state(D, kAll);
     const size_t step = (size_t)a.num_kv_heads * state;
@@ -870,16 +848,17 @@ hipError_t launch_tiles(const WindowArgs &w, hipStream_t s)
     constexpr int CG = kWaves / PS;
     const int WT = CG * (16 * kCB / (a.num_q_heads / a.num_kv_heads));
     const long long tiles = (long long)w.total_tokens / WT + a.batch, heads = a.num_kv_heads;
-    Tiling c = {0, 0, 0};
+    Tiling c = {0, -1, 0};
     if (a.batch <= kMostRequests) {
-        // Parts are fewer than twice the places (a range's n / size + 1, where n is more than size, which is more than an even share); two workgroups fit a CU.
+        // (parts are fewer than twice the places)
         const long long state = (long long)tile_state(D, CG * 16 * kCB) * (long long)sizeof(float), room = (long long)a.partial_capacity / (state + 8);
-        c.places = (int)std::min((long long)kMostPlaces, room / 2);
-        c.items = (int)std::min(room, 2LL * kMostPlaces);
+        c.log2_places = cut8::kLog2Places;
+        while (c.log2_places >= 0 && (2LL << c.log2_places) > room) --c.log2_places;
+        c.items = c.log2_places < 0 ? 0 : 2 << c.log2_places;
         // Few tiles, where a table row holds contexts that are cut.  The last part to arrive adds up: the responses 109 us, 16 tokens on 8 000 49; a second launch: 84 and 21.
-        c.later = c.places > 0 && tiles * heads < 512 && (long long)a.max_blocks * a.block_size > 32 * (2 * kLeastStages + kWorth);
+        c.later = c.log2_places >= 0 && tiles * heads < 512 && (long long)a.max_blocks * a.block_size > 32 * (2 * cut8::kLeastStages + cut8::kWorth);
     }
-    const long long grid = (tiles * heads + (c.places > 0 ? 2LL * c.places : 0) + heads - 1) / heads * heads;
+    const long long grid = (tiles * heads + c.items + heads - 1) / heads * heads;
     if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
     const bool window = w.window < (long long)a.max_blocks * a.block_size;
     if (window) hipLaunchKernelGGL((kv8_tiles<D, kCB, PS, true>), dim3((unsigned)grid), dim3(kThreads), 0, s, w, c);
@@ -887,7 +866,7 @@ hipError_t launch_tiles(const WindowArgs &w, hipStream_t s)
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !c.later) return e;
     // (a tile that is cut has two parts at least)
-    const dim3 join((unsigned)(heads * std::min(tiles, c.places / heads + 1)), CG * kCB);
+    const dim3 join((unsigned)(heads * std::min(tiles, (1LL << c.log2_places) / heads + 1)), CG * kCB);
     if (window) hipLaunchKernelGGL((kv8_join<D, kCB, CG, true>), join, dim3(kThreads), 0, s, w, c);
     else hipLaunchKernelGGL((kv8_join<D, kCB, CG, false>), join, dim3(kThreads), 0, s, w, c);
     return hipGetLastError();
@@ -924,7 +903,7 @@ hipError_t launch(const WindowArgs &w, hipStream_t s)
 size_t kv8_parts_bytes(int head_dim, int group)
 {
     if (group > 32) return 0;                            // (a wavefront per token)
-    return 2 * kMostPlaces * (tile_state(head_dim, head_dim >= 256 && group <= 16 ? 64 : 128) * sizeof(float) + 8);
+    return ((size_t)2 << cut8::kLog2Places) * (tile_state(head_dim, head_dim >= 256 && group <= 16 ? 64 : 128) * sizeof(float) + 8);
 }
 
 hipError_t launch_kv8_prefill(const WindowArgs &w, hipStream_t stream)
