@@ -52,5 +52,21 @@ __host__ __device__ inline Parts parts_of(int units, int runs)
     return Parts{each, (int)((unsigned)(units + each - 1) / (unsigned)each)};
 }
 
+// Positions that anything of a launch sees at most: a table row, or a window, the first positions, and what the other tokens of a tile see beside the first one's.
+inline long long most_seen(long long row, int window, int sinks, int tokens)
+{
+    const long long seen = (long long)window + sinks + tokens - 1;
+    return seen < row ? seen : row;
+}
+// Whether the parts of tiles of new tokens are added up by a second launch: few tiles (`tiles`: of all kv heads), where contexts may be seen that it cuts.  The last part to arrive adds
+// up: the responses 109 us, 16 tokens on 8 000 49; a second launch: 84 and 21.  (Behind a launch that cuts nothing it is time lost: 12 tokens that see the last 256 and 512 of 8 000
+// 16.4 and 20.5, without it 14.4 and 18.5.)
+inline bool tiles_later(long long tiles, long long seen) { return tiles < 1 << kLog2Places && seen > 32 * (2 * kLeastStages + kWorth); }
+// The same of one new token per request, by ranges: (request, kv head or pass).  Few, all of which may be cut: parts for one workgroup to a CU, and a second launch for the sums, whose
+// workgroups share the parts of a range: by the last of them to arrive, which is alone with them, / so, us: one request of 30 000 on 32 / 8 heads 19.6 / 17.0, 60 000 on 32 / 4 28.0 /
+// 18.1, 8 000 14.1 / 10.9, 1 999 10.0 / 9.5; 16 of 2 000 15.2 / 16.6, 200 of 100 to 4 000 on 8 / 2 heads of 64 14.8 / 21.1.  No gain where 1 024 positions at most are seen: 100 6.1 / 7.3, 700
+// 8.3 / 8.6 (all by the last / by a second launch); the last 256 of 8 000 5.9 / 8.6.
+inline bool ranges_later(long long ranges, long long seen) { return ranges < 128 && seen > 1024; }
+
 }  // namespace cut8
 }  // namespace lamps

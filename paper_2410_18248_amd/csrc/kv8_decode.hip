@@ -14,6 +14,7 @@
 #include "handover.h"
 #include "internal.h"
 #include "kv8.h"
+#include "kv8_cut.h"
 #include "requests.h"
 #include "tile_parts.h"
 #include "kv8_decode.h"
@@ -355,14 +356,10 @@ hipError_t launch(WindowArgs w, hipStream_t s)
     // Parts are no more than 5 / 3 of the places: n / size + 1 of a range, which has more than 1.5 size.  Places by what any memory for the geometry has room for (a context's and
     // lamps_decode_attn_static's), so that results go by the arguments alone.
     const size_t room = std::min((size_t)decode_max_shares(a.heads_per_pass, D) * per_share, (size_t)LAMPS_STATIC_SCRATCH_BYTES - ((size_t)1 << 20));
-    // Few ranges, all of which may be cut: parts for one workgroup to a CU, and a second launch for the sums, whose workgroups share the parts of a range: by the last of them to
-    // arrive, which is alone with them, / so, us: one request of 30 000 on 32 / 8 heads 19.6 / 17.0, 60 000 on 32 / 4 28.0 / 18.1, 8 000 14.1 / 10.9, 1 999 10.0 / 9.5;
-    // (no gain where table rows hold 1 024 positions at most: 100 6.1 / 7.3, 700 8.3 / 8.6; all by the last / by a second launch)
-    // 16 of 2 000 15.2 / 16.6, 200 of 100 to 4 000 on 8 / 2 heads of 64 14.8 / 21.1.  Otherwise 256 places, or 512 where there are hundreds of ranges (256 / 512 / 1 024: 16 of 2 000
-    // 15.2 / 16.1 / 22.6, 32 of 100 to 4 000 on 16 / 4 heads of 256 20.4 / 25.0 / 24.9; those 200 14.7 / 13.5 / 15.7, 230 of 32 to 8 192 on 32 / 8 heads 104.5 / 97.4 /
-    // 100.0).
+    // 256 places, or 512 where there are hundreds of ranges (256 / 512 / 1 024: 16 of 2 000 15.2 / 16.1 / 22.6, 32 of 100 to 4 000 on 16 / 4 heads of 256 20.4 / 25.0 / 24.9; 200 of 100 to 4 000 on
+    // 8 / 2 heads of 64 14.7 / 13.5 / 15.7, 230 of 32 to 8 192 on 32 / 8 heads 104.5 / 97.4 / 100.0).
     const long long ranges = (long long)a.batch * HC;
-    const bool later = ranges < 128 && (long long)a.max_blocks * a.block_size > 1024;
+    const bool later = cut8::ranges_later(ranges, cut8::most_seen((long long)a.max_blocks * a.block_size, w.window, w.sinks, 1));
     int log2_places = ranges < 384 ? 8 : 9;
     while (log2_places > 0 && ((size_t)2 << log2_places) * (state + 8) > room) --log2_places;
     if (((size_t)2 << log2_places) * (state + 8) > std::min(room, a.partial_capacity)) return hipErrorInvalidValue;

@@ -855,8 +855,7 @@ hipError_t launch_tiles(const WindowArgs &w, hipStream_t s)
         c.log2_places = cut8::kLog2Places;
         while (c.log2_places >= 0 && (2LL << c.log2_places) > room) --c.log2_places;
         c.items = c.log2_places < 0 ? 0 : 2 << c.log2_places;
-        // Few tiles, where a table row holds contexts that are cut.  The last part to arrive adds up: the responses 109 us, 16 tokens on 8 000 49; a second launch: 84 and 21.
-        c.later = c.log2_places >= 0 && tiles * heads < 512 && (long long)a.max_blocks * a.block_size > 32 * (2 * cut8::kLeastStages + cut8::kWorth);
+        c.later = c.log2_places >= 0 && cut8::tiles_later(tiles * heads, cut8::most_seen((long long)a.max_blocks * a.block_size, w.window, w.sinks, WT));
     }
     const long long grid = (tiles * heads + c.items + heads - 1) / heads * heads;
     if (grid > 0x7fffffffLL) return hipErrorInvalidValue;

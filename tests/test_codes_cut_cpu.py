@@ -21,6 +21,8 @@ int c_least(int size, int later) { return cut8::least_cut(size, later != 0); }
 int c_runs(int stages, int size, int worth) { return cut8::runs_of(stages, size, worth); }
 int c_next(int size) { return cut8::next_size(size); }
 int c_parts(int units, int runs, int *each) { const cut8::Parts p = cut8::parts_of(units, runs); *each = p.each; return p.count; }
+int c_tiles_later(long long tiles, long long row, int window, int sinks, int tokens) { return cut8::tiles_later(tiles, cut8::most_seen(row, window, sinks, tokens)); }
+int c_ranges_later(long long ranges, long long row, int window, int sinks) { return cut8::ranges_later(ranges, cut8::most_seen(row, window, sinks, 1)); }
 int c_tries() { return cut8::kTries; }
 }
 """
@@ -35,6 +37,8 @@ def lib(tmp_path_factory):
     lib = ctypes.CDLL(so)
     lib.c_work.restype = ctypes.c_uint64
     lib.c_size.argtypes = [ctypes.c_uint64, ctypes.c_int, ctypes.c_int]
+    lib.c_tiles_later.argtypes = [ctypes.c_longlong] * 2 + [ctypes.c_int] * 3
+    lib.c_ranges_later.argtypes = [ctypes.c_longlong] * 2 + [ctypes.c_int] * 2
     lib.c_parts.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_int)]
     return lib
 
@@ -95,6 +99,19 @@ def test_parts_of_a_tile_cover_it(lib):
             count = lib.c_parts(units, runs, ctypes.byref(each))
             assert 1 <= count <= runs and (count - 1) * each.value < units <= count * each.value
             assert count == 1 or each.value >= 4
+
+
+def test_no_second_launch_where_a_window_leaves_nothing_to_cut(lib):
+    """By what is seen, not by the table row alone; without a window by the row, as ever."""
+    all_ = 1 << 30
+    for row in (1024, 1040, 8192, 1 << 20):
+        assert lib.c_ranges_later(8, row, all_, 0) == lib.c_ranges_later(8, row, all_, all_) == (row > 1024)
+        assert lib.c_tiles_later(8, row, all_, all_, 32) == (row > 1024)
+        for window, sinks in ((1, 0), (256, 4), (512, 16), (1000, 24)):
+            assert not lib.c_ranges_later(8, row, window, sinks)
+            assert not lib.c_tiles_later(8, row, window - 1 if window > 1 else 1, sinks, 1 if window < 2 else 2)
+        assert lib.c_ranges_later(8, row, 1000, 25) == lib.c_tiles_later(8, row, 1000, 0, 26) == (row > 1024)
+    assert not lib.c_ranges_later(128, 8192, all_, 0) and not lib.c_tiles_later(512, 8192, all_, 0, 32) and lib.c_tiles_later(511, 8192, all_, 0, 32)
 
 
 def test_the_kernels_reach_the_cut_by_whole_numbers():
