@@ -195,7 +195,8 @@ size_t lamps_block_bytes(const lamps_config *cfg);
 size_t lamps_pool_bytes(const lamps_config *cfg);
 /* Bytes of device workspace the caller must allocate (256-byte aligned):
  * split partition partials (of decode calls, and of lamps_prefill_attn calls that
- * cut long contexts into runs) and the two swap staging areas. */
+ * cut long contexts into runs; LAMPS_E4M3: 68 MB of these for most geometries) and the two swap
+ * staging areas. */
 size_t lamps_workspace_bytes(const lamps_config *cfg);
 
 /* ---- life cycle ---- */
@@ -368,7 +369,8 @@ int lamps_kv_read_tokens(lamps_ctx *ctx, int32_t layer, int32_t n_req, int32_t t
  * weights); other geometries -- also pools whose blocks lie 4 GiB or more apart --
  * and any geometry when max_new_tokens < 0, run one wavefront per new token with
  * fp32 weights.  LAMPS_E4M3 is as bf16, a wavefront per token having its weights as pairs of
- * bf16 (16 bits of fraction), and leaves no row unwritten for a bound that is too small. */
+ * bf16 (16 bits of fraction), and leaves no row unwritten for a bound that is too small; with more than
+ * 256 requests no context is cut. */
 int lamps_prefill_attn(lamps_ctx *ctx, int32_t layer, int32_t n_req, int32_t total_tokens,
                        int32_t max_new_tokens, const void *q, const int32_t *q_start,
                        const int32_t *block_table, const int32_t *ctx_lens, void *out);

@@ -35,9 +35,9 @@ __host__ __device__ inline int least_cut(int size, bool later) { return later ? 
 // Parts of a tile that is cut if it has more than `worth` stages.
 __host__ __device__ inline int runs_of(int stages, int size, int worth) { return stages > worth ? (int)((unsigned)(stages + size - 1) / (unsigned)size) : 1; }
 // Where the parts are added up by a second launch they are of about one size, and the chip holds all of them at once: from an even share their size goes up until there are no
-// more of them than places (12 responses of 4 to 64 tokens on 300 to 30 000, 32 / 8 heads: 853 parts of an even share and up to half as much again, 114 us; 504 so, 84; the
-// line of all tiles in even shares, the ends of tiles in the middle of one, 90 to 96: two workgroups of a CU share what they wait for, and a tile's beginning and end cost what 8
-// stages do).
+// more of them than places (12 responses of 4 to 64 tokens on 300 to 30 000, 32 / 8 heads, by tiles that had two buffers yet: 853 parts of an even share and up to half as much again, 114 us; 504
+// so, 84; the line of all tiles in even shares, the ends of tiles in the middle of one, 90 to 96: two workgroups of a CU share what they wait for, and a tile's beginning and end cost
+// what 8 stages do).
 __host__ __device__ inline int next_size(int size) { return size + size / 16 + 1; }
 
 // Stages of each part of a tile of `units`, and parts that there are then: one of earlier tokens may have fewer stages than the request's last one, by which

@@ -8,9 +8,11 @@
 // vector ALUs).  Codes of a later stage are in registers meanwhile.  The softmax keeps a running maximum that moves only
 // where a weight would pass 2^8; weights are rounded to bf16 for the second product and summed as rounded.
 //
-// Bound, where walks are long, by the issue of products, softmax and conversions on two waves to a SIMD: 4 prompts of 4 096, 32 / 8 heads of 128, 955 to 985 us, 1.12 to 1.15 PFLOP/s, the
-// matrix cores busy 0.45 of it (a large bf16 product of the library on the same card 1.14 to 1.28; the same attention over bf16 1 010 us).  Short walks by a tile's beginning, three round
-// trips, 4 us, and its stores: 24 prompts of 16 to 700 on 40 plain heads 109 us, of which 54 are their bytes.  12 responses of 4 to 64 tokens on 300 to 30 000, 32 / 8 heads, 80 us (over bf16 571).
+// Bound, where walks are long, by the issue of products, softmax and conversions on two waves to a SIMD: 2 prompts of 8 192, 32 / 8 heads of 128, 955 to 995 us, 1.11 to 1.15 PFLOP/s, the
+// matrix cores busy 0.48 of it, the vector ALUs 0.45, LDS 0.40 (a large bf16 product of the library on the same card 1.14 to 1.28; the same attention over bf16, which has nothing to convert,
+// 880 to 910 us); 4 of 4 096 517 to 534 (475 to 494).  Short walks by a tile's beginning, three round trips, 4 us, and its stores: 24 prompts of 16 to 700 on 40 plain heads 105 to 109 us, of which 54 are
+// their bytes (over bf16 110).  12 responses of 4 to 64 tokens on 300 to 30 000, 32 / 8 heads, 78 to 81 us (over bf16 575).  Heads of 256, one product to a read of LDS: 2 prompts of 4 096, 16 / 4 heads,
+// 400 us, LDS busy 0.47 of it and the matrix cores 0.28; 4 of 1 024 84 us, 0.27 and 0.15, with 1.3 of 2 waves to a SIMD.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -32,7 +34,9 @@ struct Tiling {
     int log2_places;                                     // 2^it: workgroups that all work is dealt to evenly where requests are cut; -1: none is
     int later;                                           // parts are added up by a second launch
 };
-constexpr int kMostRequests = 256;                       // of a launch that cuts
+// Requests of a launch that cuts: a lane holds four.  (257 of 4 to 32 tokens, 32 / 8 heads, one of them 40 on 30 000: 645 us, which no other workgroup shares, where 256 take 82; by lanes that hold
+// sixteen 108, but 69 in place of 53 where all are short, and 400 of them 101 in place of 75.)
+constexpr int kMostRequests = 256;
 
 // What a workgroup takes.
 struct TilePiece {
@@ -361,7 +365,7 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
         for (int i = 0; i < SUBS; ++i) for (int k = 0; k < RING * PS; ++k) wild_at[k][kWaves * i + wv] = 0;
     }
     // A round of the walk is PS stages, one for each of the waves that share columns.  Codes are asked for a round ahead of their conversion, the first in front of the
-    // queries (two rounds ahead is no faster: 12 responses 84 us, 4 prompts of 4 096 1 008, either way).
+    // queries (two rounds ahead was no faster with two buffers: 12 responses 84 us, 2 prompts of 8 192 1 008, either way).
     Places next[PS];
     Codes codes[PS], early[RING == 4 ? 2 : 1][PS];
     const auto lookup_round = [&](int st) __attribute__((always_inline)) {
@@ -514,7 +518,7 @@ __global__ __launch_bounds__(kThreads, D >= 256 && kCB > 1 ? 1 : 2) void kv8_til
     // Operands of keys for the stage at hand are in registers where its iteration begins, those of values are asked for in front of its products
     // (heads of 256: both where they are used, for want of registers).  Behind the softmax a barrier: everyone has what the stage's buffer held, and the next one is
     // whole; the next keys are read, and a later stage is converted, while the matrix cores multiply values.  With four buffers a barrier in every second round does: the third round
-    // ahead is converted into the buffer that two rounds, and a barrier since, have left (two buffers and a barrier a round / so: 4 prompts of 4 096, 32 / 8 heads, 993 us and 970, 24 of 16 to
+    // ahead is converted into the buffer that two rounds, and a barrier since, have left (two buffers and a barrier a round / so: 2 prompts of 8 192, 32 / 8 heads, 993 us and 970, 24 of 16 to
     // 700 on 40 plain ones 115 and 111).
     bf16x8 kop[kHold ? NK : 1][2];
     uint4 vheld[kHold ? NS : 1];
