@@ -8,7 +8,7 @@
 // vector ALUs).  Codes of a later stage are in registers meanwhile.  The softmax keeps a running maximum that moves only
 // where a weight would pass 2^8; weights are rounded to bf16 for the second product and summed as rounded.
 //
-// Bound, where walks are long, by the issue of products, softmax and conversions on two waves to a SIMD: 2 prompts of 8 192, 32 / 8 heads of 128, 955 to 995 us, 1.11 to 1.15 PFLOP/s, the
+// Bound, where walks are long, by the issue of products, softmax and conversions on two waves to a SIMD: 2 prompts of 8 192, 32 / 8 heads of 128, 955 to 1 010 us by the card, 1.09 to 1.15 PFLOP/s, the
 // matrix cores busy 0.48 of it, the vector ALUs 0.45, LDS 0.40 (a large bf16 product of the library on the same card 1.14 to 1.28; the same attention over bf16, which has nothing to convert,
 // 880 to 910 us); 4 of 4 096 517 to 534 (475 to 494).  Short walks by a tile's beginning, three round trips, 4 us, and its stores: 24 prompts of 16 to 700 on 40 plain heads 105 to 109 us, of which 54 are
 // their bytes (over bf16 110).  12 responses of 4 to 64 tokens on 300 to 30 000, 32 / 8 heads, 78 to 81 us (over bf16 575).  Heads of 256, one product to a read of LDS: 2 prompts of 4 096, 16 / 4 heads,
